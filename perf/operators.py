@@ -249,11 +249,11 @@ def _own_cross_entropy(s):
     if c["kind"] == "score":
         return out
     if c["codes"]:
-        mp8.softmax_xent_bwd_fp16(M, N, K, s["x"], s["w"], s["targets"], out["lse"], dx8=out["dx"], dw8=out["dw"], dloss=s["dloss"],
+        mp8.softmax_xent_bwd_fp16(M, N, K, s["x"], s["w"], s["targets"], out["loss"], out["lse"], dx8=out["dx"], dw8=out["dw"], dloss=s["dloss"],
                                   scale=s["scale"], round=mp8.SR if c["sr"] else mp8.RNE, seed=SEED, dx_offset=1, dw_offset=2,
                                   workspace=ws)
         return {k: v.view(torch.float8_e5m2) if v.dtype == torch.uint8 else v for k, v in out.items()}
-    mp8.softmax_xent_bwd_fp16(M, N, K, s["x"], s["w"], s["targets"], out["lse"], dx16=out["dx"], dw16=out["dw"], dloss=s["dloss"],
+    mp8.softmax_xent_bwd_fp16(M, N, K, s["x"], s["w"], s["targets"], out["loss"], out["lse"], dx16=out["dx"], dw16=out["dw"], dloss=s["dloss"],
                               scale=s["scale"], workspace=ws)
     return out
 
