@@ -406,6 +406,71 @@ mp8_status mp8_wgrad_adam_fp16_sr(int64_t M, int64_t N, int64_t K, const uint8_t
                                   void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The softmax cross entropy of a language model's last layer and its gradient, from the hidden states, without the
+ * logits ever being stored (the paper keeps the last layer in 16 bits, Section 4; the loss scale of Section 3.1 enters here):
+ *     z = x [M, K] . w [N, K]^T        M tokens, N classes, K features
+ *     lse[i]  = log sum_j exp(z[i, j]);   loss[i] = lse[i] - z[i, targets[i]]
+ * and, with e[i, j] = scale * dloss[i] * (exp(z[i, j] - lse[i]) - [j = targets[i]]),
+ *     dx = e . w   [M, K]              dw = e^T . x   [N, K]
+ *   x          hidden states: IEEE halves, or 8-bit codes if x_is_e5m2 != 0; 16-byte aligned
+ *   w          IEEE halves (the master weights of the layer, or a tied embedding); 16-byte aligned
+ *   ldx, ldw   leading dimensions in elements (>= K); K, ldx and ldw best multiples of 8 (a copy of what is not, or of 8-bit x, is made)
+ *   targets    [M]; a token whose target lies outside 0 .. N-1 (padding) has loss 0 and takes no part in the gradient, whatever
+ *              its row of x holds; its lse is computed all the same
+ *   loss, lse  [M] FP32.  The loss keeps its relative precision where the target has nearly all of the probability.
+ *   dloss      nullable [M]: the weight of every token's loss (1 without it)
+ *   scale      multiplies the whole gradient: the loss scale, and 1 / tokens for a mean
+ *   dx16, dx8, dw16, dw8   each nullable, dense, 16-byte aligned: the gradients as halves (to nearest), and / or as 8-bit codes
+ *              (`round`, `flags` = MP8_FLAG_SATURATE or 0; SR uses seed, the tensor's offset and its row-major
+ *              element index).  What is not asked for is not computed; one at least is.
+ *   dx_stats, dw_stats   nullable: of the 8-bit codes, or of the halves where only those are asked for
+ *   workspace  device scratch, 16-byte aligned, mp8_softmax_xent_{fwd,bwd}_workspace_bytes(M, N, K, ldw) bytes; contents
+ *              undefined afterwards.  It grows with M * N / 16 bytes (forward) and is bounded in N backward, where the vocabulary is
+ *              taken in pieces.
+ * Precision: logits, the softmax's sums and the gradients' sums are FP32 (the products' operands halves); e is rounded to half, times a power of two
+ * that the largest token weight sets, before it is multiplied by w and x: eleven bits, which weights of less than 2^-14 of the
+ * largest lose one by one.  The results are the same from run to run.
+ * M, N <= 2^22, K <= 2^20, ldx, ldw <= 2^21 and M / 256 * N / 256 <= 2^23, rounded up (MP8_ERR_UNSUPPORTED beyond).  A zero dimension is
+ * valid and does nothing.
+ */
+mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K, const void *x, int x_is_e5m2, int64_t ldx,
+                                     const uint16_t *w, int64_t ldw, const int64_t *targets, float *loss, float *lse,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K, const void *x, int x_is_e5m2, int64_t ldx,
+                                     const uint16_t *w, int64_t ldw, const int64_t *targets, const float *loss,
+                                     const float *lse, const float *dloss, float scale, uint16_t *dx16, uint8_t *dx8,
+                                     uint16_t *dw16, uint8_t *dw8, mp8_round round, int flags, uint64_t seed,
+                                     uint64_t dx_offset, uint64_t dw_offset, mp8_stats *dx_stats, mp8_stats *dw_stats,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+size_t mp8_softmax_xent_fwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t ldw);
+size_t mp8_softmax_xent_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t ldw);
+
+/*
+ * The update path of Figure 1b with an orthogonalised momentum, for `batch` matrices [rows, cols] of weights that lie one behind the
+ * other.  Per matrix:
+ *     g  = fl32(value(g8) * inv_loss_scale);   v' = fmaf(momentum, velocity, g)
+ *     u  = v', or fmaf(momentum, v', g) if nesterov != 0
+ *     X  = u / |u|_F (0 for u = 0);  `steps` times  X <- a X + (b A + c A A) X,  A = X X^T (of the shorter side),
+ *          (a, b, c) = (3.4445, -4.7750, 2.0315): five steps bring the singular values of u to about 1, the vectors stay
+ *     w' = fmaf(-lr, fmaf(weight_decay, w, X), w);   w16 = half(w') rounded by `round` (SR uses the index in all of w16)
+ *   steps      1 .. 64
+ *   workspace  mp8_orthogonal_momentum_workspace_bytes(batch, rows, cols) bytes, 16-byte aligned, contents undefined afterwards
+ *   skip_if_nonzero  as in mp8_sgd_update_fp16_sr; a flag inside *stats is refused (MP8_ERR_INVALID_ARG), since this call
+ *              counts there while its later launches still read the flag
+ * Other arguments as for mp8_sgd_momentum_fp16_sr.  A gradient code that is Inf or NaN makes its whole matrix NaN (unless the step is
+ * skipped).  Precision: the velocity is FP32 as there; the products take half operands and add up in FP32, X is off by some 1e-3 of its
+ * root mean square (1e-2 where a few directions hold nearly all of u).  Results are the same from run to run.
+ * rows, cols <= 2^20, batch <= 65535 and batch * rows / 64 * cols / 64 <= 2^23, rounded up (MP8_ERR_UNSUPPORTED beyond).  A zero
+ * dimension is valid and does nothing.
+ */
+mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t rows, int64_t cols, uint16_t *w16, float *velocity,
+                                           const uint8_t *g8, float lr, float inv_loss_scale, float momentum, int nesterov,
+                                           float weight_decay, int steps, mp8_round round, uint64_t seed, uint64_t offset,
+                                           const uint32_t *skip_if_nonzero, uint8_t *w8_out, mp8_stats *stats,
+                                           void *workspace, size_t workspace_bytes, void *stream);
+size_t mp8_orthogonal_momentum_workspace_bytes(int64_t batch, int64_t rows, int64_t cols);
+
+/*
  * Diagnostic, for benchmarks: a kernel that only moves bytes, in the access pattern and with the
  * read:write ratio of the streaming kernels above (Section 3 calls the weight update a
  * bandwidth-bound operation; this is the stick that bound is measured with).  Reads read_bytes

@@ -35,7 +35,9 @@ EXPORTS = [
     "mp8_quantize_e5m2_batch", "mp8_wgrad_update_fp16_sr", "mp8_conv3x3_wgrad_update_fp16_sr",
     "mp8_quantize_gemm_fwd_fp8", "mp8_wgrad_momentum_fp16_sr", "mp8_conv3x3_wgrad_momentum_fp16_sr",
     "mp8_wgrad_adam_fp16_sr", "mp8_gemm_fp8_static", "mp8_static_scratch_bytes",
-    "mp8_stream_probe",
+    "mp8_stream_probe", "mp8_softmax_xent_fwd_fp16", "mp8_softmax_xent_bwd_fp16",
+    "mp8_softmax_xent_fwd_workspace_bytes", "mp8_softmax_xent_bwd_workspace_bytes",
+    "mp8_orthogonal_momentum_fp16_sr", "mp8_orthogonal_momentum_workspace_bytes",
 ]
 
 
@@ -117,6 +119,19 @@ def lib() -> C.CDLL:
     L.mp8_adam_fp16_sr.restype = ci
     L.mp8_adam_fp16_sr.argtypes = [vp, vp, vp, vp, i64, f32, f32, f32, f32, f32, f32, i64, ci, u64, u64,
                                    vp, vp, vp, vp]
+    L.mp8_softmax_xent_fwd_fp16.restype = ci
+    L.mp8_softmax_xent_fwd_fp16.argtypes = [i64, i64, i64, vp, ci, i64, vp, i64, vp, vp, vp, vp, C.c_size_t, vp]
+    L.mp8_softmax_xent_bwd_fp16.restype = ci
+    L.mp8_softmax_xent_bwd_fp16.argtypes = [i64, i64, i64, vp, ci, i64, vp, i64, vp, vp, vp, vp, f32, vp, vp, vp, vp, ci, ci,
+                                            u64, u64, u64, vp, vp, vp, C.c_size_t, vp]
+    for query in (L.mp8_softmax_xent_fwd_workspace_bytes, L.mp8_softmax_xent_bwd_workspace_bytes):
+        query.restype = C.c_size_t
+        query.argtypes = [i64, i64, i64, i64]
+    L.mp8_orthogonal_momentum_fp16_sr.restype = ci
+    L.mp8_orthogonal_momentum_fp16_sr.argtypes = [i64, i64, i64, vp, vp, vp, f32, f32, f32, ci, f32, ci, ci, u64, u64, vp, vp, vp,
+                                                  vp, C.c_size_t, vp]
+    L.mp8_orthogonal_momentum_workspace_bytes.restype = C.c_size_t
+    L.mp8_orthogonal_momentum_workspace_bytes.argtypes = [i64, i64, i64]
     L.mp8_stream_probe.restype = ci
     L.mp8_stream_probe.argtypes = [vp, vp, i64, ci, vp]
     L.mp8_sr_bits.restype = ci
@@ -411,6 +426,43 @@ def adam_fp16_sr(w16, m, v, g8, lr, inv_loss_scale, step, beta1=0.9, beta2=0.999
     (_nat or _native()).adam_fp16_sr(w16, m, v, g8, lr, inv_loss_scale, step, beta1, beta2, eps, weight_decay, round, seed,
                                      offset, skip_if_nonzero, w8_out, stats)
     return w16
+
+
+def orthogonal_momentum_workspace_bytes(batch, rows, cols) -> int:
+    return int(lib().mp8_orthogonal_momentum_workspace_bytes(batch, rows, cols))
+
+
+def orthogonal_momentum_fp16_sr(w16, velocity, g8, lr, inv_loss_scale, momentum, nesterov=True, weight_decay=0.0, steps=5,
+                                round=SR, seed=0, offset=0, skip_if_nonzero=None, w8_out=None, stats=None, workspace=None):
+    """mp8_orthogonal_momentum_fp16_sr: momentum whose direction is orthogonalised (Newton-Schulz) before it is applied to the
+    float16 master weights w16 [..., rows, cols]; FP32 velocity in place."""
+    (_nat or _native()).orthogonal_momentum_fp16_sr(w16, velocity, g8, lr, inv_loss_scale, momentum, nesterov, weight_decay, steps, round,
+                                                    seed, offset, skip_if_nonzero, w8_out, stats, workspace)
+    return w16
+
+
+def softmax_xent_fwd_workspace_bytes(M, N, K, ldw=None) -> int:
+    return int(lib().mp8_softmax_xent_fwd_workspace_bytes(M, N, K, K if ldw is None else ldw))
+
+
+def softmax_xent_bwd_workspace_bytes(M, N, K, ldw=None) -> int:
+    return int(lib().mp8_softmax_xent_bwd_workspace_bytes(M, N, K, K if ldw is None else ldw))
+
+
+def softmax_xent_fwd_fp16(M, N, K, x, w, targets, loss, lse, workspace=None, ldx=None, ldw=None):
+    """mp8_softmax_xent_fwd_fp16: loss and lse [M] of the logits x [M, K] . w [N, K]^T, which are not stored.  x is
+    float16 or uint8 (8-bit codes), w float16, targets int64 (outside 0 .. N-1: no target)."""
+    (_nat or _native()).softmax_xent_fwd_fp16(M, N, K, x, w, targets, ldx, ldw, loss, lse, workspace)
+    return loss
+
+
+def softmax_xent_bwd_fp16(M, N, K, x, w, targets, loss, lse, dx16=None, dx8=None, dw16=None, dw8=None, dloss=None, scale=1.0,
+                          round=RNE, flags=0, seed=0, dx_offset=0, dw_offset=0, dx_stats=None, dw_stats=None, workspace=None,
+                          ldx=None, ldw=None):
+    """mp8_softmax_xent_bwd_fp16: the gradient of sum(scale * dloss * loss) by x and w, as float16 and / or 8-bit codes, from
+    the loss and lse of softmax_xent_fwd_fp16."""
+    (_nat or _native()).softmax_xent_bwd_fp16(M, N, K, x, w, targets, ldx, ldw, loss, lse, dloss, scale, dx16, dx8, dw16, dw8, round, flags,
+                                              seed, dx_offset, dw_offset, dx_stats, dw_stats, workspace)
 
 
 def sr_bits(out, seed=0, offset=0):

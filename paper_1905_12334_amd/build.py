@@ -10,7 +10,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmp8.so")
-SOURCES = ["quantize.hip", "update.hip", "gemm.hip", "host.hip"]
+SOURCES = ["quantize.hip", "update.hip", "gemm.hip", "xent.hip", "ortho.hip", "host.hip"]
 # -ffp-contract=off: every multiply and add is rounded on its own (the one fused operation,
 # the weight update, is an explicit fma).  Packed FP32 instructions are switched off.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",

@@ -15,6 +15,7 @@
 #include <cstdarg>
 #include <cstring>
 #include <exception>
+#include <initializer_list>
 
 #include "../../include/mp8.h"
 
@@ -27,7 +28,8 @@ PyObject *g_error = nullptr;  // Mp8Error
     X(mp8_quantize_e5m2) X(mp8_gemm_fp8_tuned) X(mp8_gemm_fp8_static) X(mp8_quantize_gemm_fwd_fp8)   \
     X(mp8_conv3x3_fp8) X(mp8_conv3x3_wgrad_update_fp16_sr) X(mp8_conv3x3_wgrad_momentum_fp16_sr)     \
     X(mp8_wgrad_update_fp16_sr) X(mp8_wgrad_momentum_fp16_sr) X(mp8_wgrad_adam_fp16_sr)              \
-    X(mp8_sgd_update_fp16_sr) X(mp8_sgd_momentum_fp16_sr) X(mp8_adam_fp16_sr) X(mp8_status_string)
+    X(mp8_sgd_update_fp16_sr) X(mp8_sgd_momentum_fp16_sr) X(mp8_adam_fp16_sr) X(mp8_status_string)        \
+    X(mp8_softmax_xent_fwd_fp16) X(mp8_softmax_xent_bwd_fp16) X(mp8_orthogonal_momentum_fp16_sr)
 #define MP8_POINTER(name) decltype(&name) p_##name = nullptr;
 MP8_ENTRIES(MP8_POINTER)
 #undef MP8_POINTER
@@ -44,7 +46,8 @@ struct Raised {};
 }
 
 // What a tensor argument may hold.
-enum Kind { kF32, kU8, kSource /* float32 or float16 */, kHalf /* float16 or its bits */ };
+enum Kind { kF32, kU8, kSource /* float32 or float16 */, kHalf /* float16 or its bits */,
+            kHidden /* float16, or 8-bit codes */, kI64 };
 
 struct Arg {
     void *p = nullptr;
@@ -160,6 +163,8 @@ struct Args {
                 ok = s == at::kHalf || s == at::kShort || s == at::kUInt16;
                 expected = "(torch.float16, torch.int16, torch.uint16)";
                 break;
+            case kHidden: ok = s == at::kHalf || s == at::kByte; expected = "(torch.float16, torch.uint8)"; break;
+            case kI64: ok = s == at::kLong; expected = "torch.int64"; break;
         }
         if (!ok) {
             PyObject *d = PyObject_GetAttrString(o, "dtype");
@@ -560,6 +565,104 @@ void update(Args a) {
         }), "mp8_adam_fp16_sr");
 }
 
+// Every tensor given lies on the current device, whose stream the call goes to.
+void on_current_device(std::initializer_list<const Arg *> args) {
+    const int current = c10::hip::current_device();
+    for (const Arg *x : args)
+        if (x->given && x->t != nullptr && x->t->is_cuda() && x->t->get_device() != current)
+            fail("a tensor lies on another device than the current one");
+}
+
+// The operands both directions share.
+struct XentArgs {
+    int64_t M, N, K, ldx, ldw;
+    Arg x, w, targets;
+    explicit XentArgs(Args &a) : M(a.i64()), N(a.i64()), K(a.i64()) {
+        x = a.tensor("x", kHidden);
+        w = a.tensor("w", kHalf);
+        targets = a.tensor("targets", kI64);
+        ldx = a.i64_or(K);
+        ldw = a.i64_or(K);
+        must_be(x, "x");
+        must_be(w, "w");
+        must_be(targets, "targets");
+        exactly(targets, M, "targets", "M");
+        at_least(x, span(false, M, K, ldx), "x", "its shape and leading dimension require");
+        at_least(w, span(false, N, K, ldw), "w", "its shape and leading dimension require");
+    }
+    int codes() const { return x.t->scalar_type() == at::kByte; }
+};
+
+void softmax_xent_fwd(Args a) {
+    const XentArgs d(a);
+    const Arg loss = a.tensor("loss", kF32), lse = a.tensor("lse", kF32), ws = a.raw(true);
+    must_be(loss, "loss");
+    must_be(lse, "lse");
+    exactly(loss, d.M, "loss", "M");
+    exactly(lse, d.M, "lse", "M");
+    on_current_device({&d.x, &d.w, &d.targets, &loss, &lse, &ws});
+    const size_t ws_bytes = a.bytes(ws);
+    void *s = stream();
+    check(unlocked([&] {
+        return p_mp8_softmax_xent_fwd_fp16(d.M, d.N, d.K, d.x.p, d.codes(), d.ldx, (const uint16_t *)d.w.p, d.ldw, (const int64_t *)d.targets.p,
+                                           (float *)loss.p, (float *)lse.p, ws.p, ws_bytes, s);
+    }), "mp8_softmax_xent_fwd_fp16");
+}
+
+void softmax_xent_bwd(Args a) {
+    const XentArgs d(a);
+    const Arg loss = a.tensor("loss", kF32), lse = a.tensor("lse", kF32), dloss = a.tensor("dloss", kF32);
+    const float scale = a.f32();
+    const Arg dx16 = a.tensor("dx16", kHalf), dx8 = a.tensor("dx8", kU8), dw16 = a.tensor("dw16", kHalf), dw8 = a.tensor("dw8", kU8);
+    const int round = a.i32(), flags = a.i32();
+    const uint64_t seed = a.u64(), dx_offset = a.u64(), dw_offset = a.u64();
+    const Arg dx_stats = a.raw(), dw_stats = a.raw(), ws = a.raw(true);
+    must_be(loss, "loss");
+    must_be(lse, "lse");
+    exactly(loss, d.M, "loss", "M");
+    exactly(lse, d.M, "lse", "M");
+    exactly(dloss, d.M, "dloss", "M");
+    exactly(dx16, mul(d.M, d.K), "dx16", "M*K");
+    exactly(dx8, mul(d.M, d.K), "dx8", "M*K");
+    exactly(dw16, mul(d.N, d.K), "dw16", "N*K");
+    exactly(dw8, mul(d.N, d.K), "dw8", "N*K");
+    on_current_device({&d.x, &d.w, &d.targets, &loss, &lse, &dloss, &dx16, &dx8, &dw16, &dw8, &dx_stats, &dw_stats, &ws});
+    const size_t ws_bytes = a.bytes(ws);
+    void *s = stream();
+    check(unlocked([&] {
+        return p_mp8_softmax_xent_bwd_fp16(d.M, d.N, d.K, d.x.p, d.codes(), d.ldx, (const uint16_t *)d.w.p, d.ldw, (const int64_t *)d.targets.p,
+                                           (const float *)loss.p, (const float *)lse.p, (const float *)dloss.p, scale, (uint16_t *)dx16.p,
+                                           (uint8_t *)dx8.p, (uint16_t *)dw16.p, (uint8_t *)dw8.p, (mp8_round)round, flags, seed, dx_offset,
+                                           dw_offset, (mp8_stats *)dx_stats.p, (mp8_stats *)dw_stats.p, ws.p, ws_bytes, s);
+    }), "mp8_softmax_xent_bwd_fp16");
+}
+
+void orthogonal_momentum(Args a) {
+    const Arg w16 = a.tensor("w16", kHalf), vel = a.tensor("velocity", kF32), g8 = a.tensor("g8", kU8);
+    const float lr = a.f32(), inv = a.f32(), mu = a.f32();
+    const int nesterov = a.flag();
+    const float wd = a.f32();
+    const int steps = a.i32(), round = a.i32();
+    const uint64_t seed = a.u64(), offset = a.u64();
+    const Arg skip = a.raw(), w8 = a.tensor("w8_out", kU8), stats = a.raw(), ws = a.raw(true);
+    must_be(w16, "w16");
+    must_be(vel, "velocity");
+    must_be(g8, "g8");
+    if (w16.t->dim() < 2) fail("w16 must be a matrix or a batch of them");
+    if (g8.n != w16.n || vel.n != w16.n || (w8 && w8.n != w16.n)) fail("velocity / g8 / w8_out size does not match w16");
+    on_current_device({&w16, &vel, &g8, &skip, &w8, &stats, &ws});
+    const int64_t rows = w16.t->size(-2), cols = w16.t->size(-1);
+    int64_t batch = 1;
+    for (int64_t k = 0; k + 2 < w16.t->dim(); ++k) batch = mul(batch, w16.t->size(k));
+    const size_t ws_bytes = a.bytes(ws);
+    void *s = stream();
+    check(unlocked([&] {
+        return p_mp8_orthogonal_momentum_fp16_sr(batch, rows, cols, (uint16_t *)w16.p, (float *)vel.p, (const uint8_t *)g8.p, lr, inv, mu,
+                                                 nesterov, wd, steps, (mp8_round)round, seed, offset, (const uint32_t *)skip.p, (uint8_t *)w8.p,
+                                                 (mp8_stats *)stats.p, ws.p, ws_bytes, s);
+    }), "mp8_orthogonal_momentum_fp16_sr");
+}
+
 template <void (*F)(Args)>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
     try {
@@ -609,6 +712,9 @@ PyMethodDef kMethods[] = {
     MP8_METHOD("sgd_update_fp16_sr", update<0>),
     MP8_METHOD("sgd_momentum_fp16_sr", update<1>),
     MP8_METHOD("adam_fp16_sr", update<2>),
+    MP8_METHOD("softmax_xent_fwd_fp16", softmax_xent_fwd),
+    MP8_METHOD("softmax_xent_bwd_fp16", softmax_xent_bwd),
+    MP8_METHOD("orthogonal_momentum_fp16_sr", orthogonal_momentum),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

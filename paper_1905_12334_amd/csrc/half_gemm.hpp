@@ -1,0 +1,333 @@
+// Products of half-precision matrices, out[r, c] = sum_j a[r, j] b[c, j], FP32 accumulation, on the half-precision matrix
+// instruction, with what becomes of a finished FP32 tile left to the caller (Epi): the softmax's statistics or its gradient
+// (xent.hip), a Gram matrix, a polynomial of it or the next iterate (ortho.hip).
+#pragma once
+
+#include "gemm_common.hpp"
+
+namespace mp8 {
+
+// An operand is stored with its contraction index contiguous ([rows, kc]), or contraction-major ([kc, rows]).  Leading dimensions and
+// batch strides in bytes; addresses and both are multiples of 16.  A row-major operand is read to the next multiple of 8 of its
+// contraction, where it has to hold zeros (or finite values, if the other operand holds zeros there); a contraction-major one has a
+// multiple of 8 rows.
+struct HalfGemm {
+    const uint8_t *a, *b;
+    int64_t lda, ldb, a_batch, b_batch;
+    int rows, cols;      // of the output; loads beyond them are clamped to the last row (or eight rows), and never stored
+    int ksteps, tail;    // stages of 64, and the contraction indices of a last, incomplete one (0: none; see GemmArgs::tail)
+    int splits, ks_per, ks_extra;
+    int tiles_m, tiles_n;
+    int symmetric;       // square output of which only the tiles on and above the diagonal are made
+    const uint32_t *skip;  // nullable: a call that is skipped if this is not zero
+    FastDiv div_tiles;   // by the tiles of one slice
+    FastDiv div_splits;
+    FastDiv div_band, div_last, div_tn;  // by 8 * tiles_n, by the height of the last band of 8 tile rows, by tiles_n
+};
+
+// Which part of the output a workgroup makes.
+struct HalfTile {
+    int batch, split, tm, tn;
+};
+
+// Consecutive workgroups go to different XCDs, each with an L2 of its own: workgroup i takes the i/8-th tile of the i%8-th eighth of
+// them, so that what runs on one XCD is a run of neighbours, in bands of eight tile rows.
+__device__ __forceinline__ HalfTile half_tile(const HalfGemm &p) {
+    const uint32_t n = gridDim.x, i = blockIdx.x, q = n >> 3, r = n & 7, x = i & 7;
+    uint32_t id = x * q + (x < r ? x : r) + (i >> 3);
+    HalfTile t;
+    uint32_t tile, split;
+    id = fastdiv(id, p.div_tiles, tile);
+    t.batch = (int)fastdiv(id, p.div_splits, split);
+    t.split = (int)split;
+    if (p.symmetric) {
+        // row i of the upper triangle starts at i (2 T - i + 1) / 2; counted from the end, row T - 1 - k has k + 1 tiles
+        const uint32_t T = (uint32_t)p.tiles_m, back = T * (T + 1) / 2 - 1 - tile;
+        uint32_t k = (uint32_t)((__builtin_sqrtf(8.0f * (float)back + 1.0f) - 1.0f) * 0.5f);
+        if (k * (k + 1) / 2 > back) --k;
+        if ((k + 1) * (k + 2) / 2 <= back) ++k;
+        t.tm = (int)(T - 1 - k);
+        t.tn = (int)(T - 1 - (back - k * (k + 1) / 2));
+    } else {
+        uint32_t in_band, y;
+        const uint32_t band = fastdiv(tile, p.div_band, in_band);
+        const uint32_t left = (uint32_t)p.tiles_m - 8 * band;
+        if (left >= 8) {
+            t.tn = (int)(in_band >> 3);
+            y = in_band & 7;
+        } else {
+            t.tn = (int)fastdiv(in_band, p.div_last, y);
+        }
+        t.tm = (int)(8 * band + y);
+    }
+    t.batch = __builtin_amdgcn_readfirstlane(t.batch);
+    t.split = __builtin_amdgcn_readfirstlane(t.split);
+    t.tm = __builtin_amdgcn_readfirstlane(t.tm);
+    t.tn = __builtin_amdgcn_readfirstlane(t.tn);
+    return t;
+}
+
+// Tiles: four waves, WGM x WGN of them, each with a grid of 32x32 accumulators.
+template <int BM_, int BN_, int NSTAGE_, int MINBLOCKS_>
+struct HalfTiling {
+    static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = 2, NSTAGE = NSTAGE_, MINBLOCKS = MINBLOCKS_;
+    static constexpr int WTM = BM / WGM, WTN = BN / WGN, MT = WTM / 32, NT = WTN / 32;
+};
+using f32x2 = float __attribute__((ext_vector_type(2)));
+using Half256 = HalfTiling<256, 256, 2, 1>;
+using Half128 = HalfTiling<128, 128, 2, 2>;
+using Half64 = HalfTiling<64, 64, 4, 2>;
+
+// Where a lane's accumulators lie.  Element e of accumulator (i, j) is row row(i), column col(j) + 8 (e / 4) + e % 4.
+template <class T>
+struct HalfPlace {
+    int batch, split, tm, tn;
+    int row0, col0;  // of the wave's part
+    int wave, lane;
+    __device__ __forceinline__ int row(int i) const { return row0 + 32 * i + (lane & 31); }
+    __device__ __forceinline__ int col(int j) const { return col0 + 32 * j + 4 * (lane >> 5); }
+};
+
+// The pipeline is the one of gemm_mfma_kernel (a ring of 128-byte-wide operand slabs in LDS, direct-to-LDS loads, one barrier per
+// stage, fragments fetched one sub-step ahead, everything between two matrix instructions), with four sub-steps of sixteen
+// contraction indices per stage: the barrier stands behind the third, by which all fragments of the stage have
+// been read.  Slab images:
+//   row-major: row r is 128 bytes, its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7)
+//   contraction-major: panels of 64 tile rows; 64 contraction rows of 128 bytes, chunk c of contraction row k in slot
+//     c ^ (4 ((k >> 1) & 1)).  The transposing read names 4 x 4 halves per 16 lanes: lanes 0 .. 31 read four contraction
+//     rows of four chunks, which this swizzle spreads over all 64 banks.
+template <class T, bool ATN, bool BTN, class Epi>
+__global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const HalfGemm p, const Epi epi) {
+    constexpr int BM = T::BM, BN = T::BN, WTM = T::WTM, WTN = T::WTN, MT = T::MT, NT = T::NT, NSTAGE = T::NSTAGE;
+    constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+    constexpr int A_DMA = BM / 32, B_DMA = BN / 32, G = A_DMA + B_DMA;  // direct loads per wave and stage
+    constexpr int F = MT + NT, NM = MT * NT;                             // fragments and matrix instructions per sub-step
+    static_assert(G * (NSTAGE - 1) < 64, "vmcnt range");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NSTAGE * STAGE];
+
+    if (p.skip != nullptr && *p.skip != 0u) return;
+    const HalfTile tile = half_tile(p);
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / T::WGN, wn = wave % T::WGN;
+    const int row0 = tile.tm * BM, col0 = tile.tn * BN;
+    const int ks_begin = tile.split * p.ks_per + (tile.split < p.ks_extra ? tile.split : p.ks_extra);
+    const int ks_count = __builtin_amdgcn_readfirstlane(p.ks_per + (tile.split < p.ks_extra ? 1 : 0));
+
+    const bool has_tail = p.tail != 0;
+    const int first = ks_begin - (has_tail ? 1 : 0);  // stage s of this slice covers indices 64 (first + s) ..
+    const int64_t a_kstep = ATN ? 64 * p.lda : 128, b_kstep = BTN ? 64 * p.ldb : 128;
+    const uint8_t *a_tile = uniform_ptr(p.a + tile.batch * p.a_batch + (ATN ? 2 * (int64_t)row0 : row0 * p.lda) + first * a_kstep);
+    const uint8_t *b_tile = uniform_ptr(p.b + tile.batch * p.b_batch + (BTN ? 2 * (int64_t)col0 : col0 * p.ldb) + first * b_kstep);
+
+    // load q of this wave: the slab's KB u = wave + 4 q
+    auto krow = [&](int q) { return 8 * ((wave + 4 * q) & 7) + (lane >> 3); };  // contraction-major: of the stage's 64
+    const int lchunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7), lchunk_t = (lane & 7) ^ (((lane >> 4) & 1) << 2);
+    auto offset = [&](bool km, int q, int origin, int extent, int64_t ld) -> uint32_t {
+        if (km) {
+            int m = 64 * ((wave + 4 * q) >> 3) + 8 * lchunk_t;
+            m = origin + m + 8 <= extent ? m : extent - 8 - origin;
+            return (uint32_t)(krow(q) * ld + 2 * m);
+        }
+        int r = 8 * (wave + 4 * q) + (lane >> 3);
+        r = origin + r < extent ? r : extent - 1 - origin;
+        return (uint32_t)(r * ld) + 16 * lchunk;
+    };
+    uint32_t oa[A_DMA], ob[B_DMA];
+#pragma unroll
+    for (int q = 0; q < A_DMA; ++q) oa[q] = offset(ATN, q, row0, p.rows, p.lda);
+#pragma unroll
+    for (int q = 0; q < B_DMA; ++q) ob[q] = offset(BTN, q, col0, p.cols, p.ldb);
+    const uint32_t lds0 = lds_address(lds);
+    auto issue_one = [&](int s, int q) {  // load q (0 .. G-1) of stage s
+        const uint32_t at = lds0 + (s % NSTAGE) * STAGE + wave * 1024;
+        if (q < A_DMA) dma16(a_tile + s * a_kstep, oa[q < A_DMA ? q : 0], at + q * 4096);
+        else dma16(b_tile + s * b_kstep, ob[q >= A_DMA ? q - A_DMA : 0], at + A_BYTES + (q - A_DMA) * 4096);
+    };
+    // the incomplete stage (stage 0 of the first slice): the contraction's last indices, and zeros
+    auto issue_tail = [&]() {
+        const uint32_t at = lds0 + wave * 1024;
+        const uint8_t *ak = a_tile + (int64_t)p.ksteps * a_kstep, *bk = b_tile + (int64_t)p.ksteps * b_kstep;
+        auto inside = [&](bool km, int q) { return (km ? krow(q) : 8 * lchunk) < p.tail; };
+#pragma unroll
+        for (int q = 0; q < A_DMA; ++q) dma16_or_zero(ak, oa[q], inside(ATN, q), at + q * 4096);
+#pragma unroll
+        for (int q = 0; q < B_DMA; ++q) dma16_or_zero(bk, ob[q], inside(BTN, q), at + A_BYTES + q * 4096);
+    };
+
+    // Fragment f of sub-step `sub`: lane l holds contraction indices 16 sub + 8 (l / 32) .. +7 of tile row l % 32 of
+    // A tile f (f < MT) or B tile f - MT.
+    const int frow = lane & 31, fk = lane >> 5, fsw = (frow >> 1) & 7, t16 = lane & 15;
+    const int kt = 8 * fk + (t16 >> 2);                                  // transposing reads: this lane's contraction row
+    const int ct = ((lane >> 4) & 1) * 2 + ((t16 & 3) >> 1);             // and chunk
+    const int ft = kt * 128 + ((ct ^ (((t16 >> 3) & 1) << 2)) << 4) + 8 * (t16 & 1);
+    auto fragment = [&](int s, int sub, int f) -> half8 {
+        const uint8_t *slab = lds + (s % NSTAGE) * STAGE + (f < MT ? 0 : A_BYTES);
+        const int m = f < MT ? wm * WTM + 32 * f : wn * WTN + 32 * (f - MT);
+        if ((f < MT && ATN) || (f >= MT && BTN)) {
+            using h4 = short __attribute__((ext_vector_type(4)));
+            using lds_h4 = __attribute__((address_space(3))) h4;
+            // (the panel's upper 32 tile rows are chunks 4 .. 7: the other value of the swizzled bit)
+            const uint8_t *at = slab + (m >> 6) * 8192 + (ft ^ ((m & 32) << 1)) + 16 * sub * 128;
+            const h4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4 *)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4 *)(at + 512));
+            return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+        return *reinterpret_cast<const half8 *>(slab + (m + frow) * 128 + (((2 * sub + fk) ^ fsw) << 4));
+    };
+    auto order = [&](int n) { return n == 0 ? MT : n == 1 ? 0 : n < NT + 1 ? MT + n - 1 : n - NT; };  // as first needed
+
+    f32x16 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+    auto wait_stage = [&](int s) {  // stage s has landed; later ones may be under way
+        int later = ks_count - 1 - s;
+        later = later < NSTAGE - 2 ? later : NSTAGE - 2;
+        if (NSTAGE > 2 && later >= NSTAGE - 2) wait_vm_lds<G * (NSTAGE - 2)>();
+        else if (NSTAGE > 3 && later == 1) wait_vm_lds<G>();
+        else wait_vm_lds<0>();
+    };
+    half8 fr[2][F];
+#pragma unroll
+    for (int s = 0; s < NSTAGE; ++s)
+        if (s < ks_count) {
+            if (s == 0 && has_tail && ks_begin == 0) issue_tail();
+            else
+#pragma unroll
+                for (int q = 0; q < G; ++q) issue_one(s, q);
+        }
+    // (the whole ring has been issued: up to NSTAGE - 1 stages lie behind the first)
+    if (ks_count >= NSTAGE) wait_vm_lds<G * (NSTAGE - 1)>();
+    else if (NSTAGE > 3 && ks_count == 3) wait_vm_lds<2 * G>();
+    else if (NSTAGE > 2 && ks_count == 2) wait_vm_lds<G>();
+    else wait_vm_lds<0>();
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < F; ++n) fr[0][order(n)] = fragment(0, 0, order(n));
+    constexpr int R = (F + NM - 1) / NM, D = (G + NM - 1) / NM;  // fragment reads and loads per matrix instruction
+    for (int t = 0; t < ks_count; ++t) {
+        const bool more = t + NSTAGE < ks_count, next = t + 1 < ks_count;
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub) {
+#pragma unroll
+            for (int k = 0; k < NM; ++k) {
+                const int i = k / NT, j = k % NT;
+                // b goes in as the "row" matrix so that a lane ends up with consecutive output columns
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[sub & 1][MT + j], fr[sub & 1][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int n = k * R + r;
+                    if (n < F && (sub < 3 || next)) fr[(sub + 1) & 1][order(n)] = fragment(sub < 3 ? t : t + 1, (sub + 1) & 3, order(n));
+                }
+                if (sub == 3 && more) {
+#pragma unroll
+                    for (int r = 0; r < D; ++r)
+                        if (k * D + r < G) issue_one(t + NSTAGE, k * D + r);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (sub == 2) {
+                if (next) wait_stage(t + 1);
+                else wait_vm_lds<63>();
+                __syncthreads();
+            }
+        }
+    }
+    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane};
+    epi(at, acc);
+}
+
+// Sixteen columns of accumulator elements 4 g .. 4 g + 7 (g even), packed as halves: the lower half wave ends up with columns
+// 8 g .. +7 of the 32, the upper one with the eight after them, sixteen bytes each.
+__device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const half2v h = {(_Float16)v[2 * q], (_Float16)v[2 * q + 1]};
+        w[q] = __builtin_bit_cast(uint32_t, h);
+    }
+    const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    return u32x4{s0[0], s1[0], s0[1], s1[1]};
+}
+
+// The FP32 tile itself, scaled by nothing, stored or added to what is there: slab `split` of [rows, ld] floats (ld a multiple of
+// 32 and at least the columns, so that whole rows of 32 may be stored).
+struct HalfEpiSum {
+    float *out;
+    int64_t ld, slab, batch;  // in floats
+    int rows, cols, add;
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        float *base = out + at.batch * batch + at.split * slab;
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            const int r = at.row(i);
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j) {
+                if (at.col0 + 32 * j >= cols) break;
+#pragma unroll
+                for (int g = 0; g < 4; g += 2) {
+                    f32x4 lo, hi;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const auto s = __builtin_amdgcn_permlane32_swap(f2u(acc[i][j][4 * g + e]), f2u(acc[i][j][4 * g + 4 + e]), false, false);
+                        lo[e] = u2f(s[0]);
+                        hi[e] = u2f(s[1]);
+                    }
+                    if (r < rows) {
+                        f32x4 *to = reinterpret_cast<f32x4 *>(base + r * ld + at.col0 + 32 * j + 8 * g + 8 * (at.lane >> 5));
+                        if (add) {
+                            lo += to[0];
+                            hi += to[1];
+                        }
+                        to[0] = lo;
+                        to[1] = hi;
+                    }
+                }
+            }
+        }
+    }
+};
+
+// Host side: the geometry of a call.  Sizes have been checked: rows, cols, kc >= 1 and what HalfGemm says.
+static inline HalfGemm half_gemm_args(const void *a, int64_t lda, int64_t a_batch, const void *b, int64_t ldb, int64_t b_batch, int64_t rows,
+                                      int64_t cols, int64_t kc, int tile_m, int tile_n, int splits, bool symmetric) {
+    HalfGemm p{};
+    p.a = (const uint8_t *)a;
+    p.b = (const uint8_t *)b;
+    p.lda = 2 * lda;
+    p.ldb = 2 * ldb;
+    p.a_batch = 2 * a_batch;
+    p.b_batch = 2 * b_batch;
+    p.rows = (int)rows;
+    p.cols = (int)cols;
+    p.ksteps = (int)((kc + 63) / 64);
+    p.tail = (int)(kc % 64);
+    p.splits = splits;
+    p.ks_per = p.ksteps / splits;
+    p.ks_extra = p.ksteps % splits;
+    p.tiles_m = (int)((rows + tile_m - 1) / tile_m);
+    p.tiles_n = (int)((cols + tile_n - 1) / tile_n);
+    p.symmetric = symmetric;
+    const int tiles = symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    p.div_tiles = make_fastdiv((uint32_t)tiles);
+    p.div_splits = make_fastdiv((uint32_t)splits);
+    p.div_band = make_fastdiv((uint32_t)(8 * p.tiles_n));
+    p.div_last = make_fastdiv((uint32_t)(p.tiles_m % 8 ? p.tiles_m % 8 : 8));
+    p.div_tn = make_fastdiv((uint32_t)p.tiles_n);
+    return p;
+}
+
+template <class T, bool ATN, bool BTN, class Epi>
+static inline bool half_gemm_launch(const HalfGemm &p, int64_t batch, const Epi &epi, hipStream_t stream) {
+    const int64_t tiles = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
+    hipLaunchKernelGGL((half_gemm_kernel<T, ATN, BTN, Epi>), dim3((unsigned)(tiles * p.splits * batch)), dim3(256), 0, stream, p, epi);
+    return hipGetLastError() == hipSuccess;
+}
+
+}  // namespace mp8

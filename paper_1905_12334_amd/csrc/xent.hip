@@ -1,0 +1,542 @@
+// Softmax cross entropy of a last layer's logits z = x . w^T (M tokens, N classes, K features) and its gradient, on the
+// half-precision matrix instruction.  Section 4 of arXiv 1905.12334 keeps the last layer in 16 bits; the error that its
+// backward pass hands down is where the loss scale of Section 3.1 enters.
+//
+//   forward   m = max_j z_ij,  lse_i = m + log sum_j exp(z_ij - m),  loss_i = lse_i - z_it
+//   backward  e_ij = scale dloss_i (exp(z_ij - lse_i) - [j = t]),  dx = e . w,  dw = e^T . x
+//
+// The logits are never stored.  The forward pass reduces every tile of them to a maximum and a sum per row, and a second kernel joins these.
+// The backward pass makes the logits once more, a piece of the vocabulary at a time, stores e of that piece as halves and
+// multiplies it by w (added up over the pieces in FP32) and x (complete per piece).
+#include <cmath>
+
+#include "half_gemm.hpp"
+
+namespace mp8 {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr double kLn2 = 0.69314718055994530942;
+// e is stored times 2^14: values of up to 1 in magnitude fill the half format from its top, and a probability keeps eleven bits
+// down to 2^-28 and an absolute precision of 2^-39 below.
+constexpr int kErrorExponent = 14;
+
+// ---------------------------------------------------------------------------------------
+// What becomes of a tile of logits.
+// ---------------------------------------------------------------------------------------
+// Sums are of powers of two: with base B = fl(m log2 e), sum 2^(z log2 e - B), one rounding per exponent (a fused multiply-add);
+// what B itself was rounded by cancels when the sums are joined.  The target's logit is kept apart: the loss is
+// log(1 + what the others have beside it), which lse - z would not give where the target has nearly everything.
+struct XentStats {
+    const int64_t *targets;
+    f32x2 *part;     // [parts, M]: (B, sum) of the columns of one wave's tile, without the target
+    float *z_target; // [M]
+    int M, N, first; // `first`: class of this piece's column 0
+    int part0;       // of this piece
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        const int h4 = 4 * (at.lane >> 5), left = N - at.col0;  // columns of this wave's tile that exist
+        if (left <= 0) return;
+        int64_t target[T::MT];
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) target[i] = at.row(i) < M ? targets[at.row(i)] : -1;
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            f32x16 (&z)[T::NT] = acc[i];
+            if (left < T::WTN) {
+#pragma unroll
+                for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (32 * j + 8 * (e >> 2) + h4 + (e & 3) >= left) z[j][e] = -__builtin_inff();
+            }
+            const int64_t rel = target[i] - first - at.col0;
+            const bool here = rel >= 0 && rel < T::WTN && rel < left;
+            if (__builtin_amdgcn_ballot_w64(here) != 0) {
+                const int c = here ? (int)rel - h4 : -1;
+#pragma unroll
+                for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (c == 32 * j + 8 * (e >> 2) + (e & 3)) {
+                            z_target[at.row(i)] = z[j][e];
+                            z[j][e] = -__builtin_inff();
+                        }
+            }
+            float m = -__builtin_inff();
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) m = __builtin_fmaxf(m, z[j][e]);
+            const auto both = __builtin_amdgcn_permlane32_swap(f2u(m), f2u(m), false, false);
+            m = __builtin_fmaxf(u2f(both[0]), u2f(both[1]));
+            const float base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
+            float s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base));
+            const auto sums = __builtin_amdgcn_permlane32_swap(f2u(s), f2u(s), false, false);
+            s = u2f(sums[0]) + u2f(sums[1]);
+            const int r = at.row(i);
+            if (at.lane < 32 && r < M) part[(int64_t)(part0 + at.col0 / T::WTN) * M + r] = f32x2{base, s};
+        }
+    }
+};
+
+// e of a tile, as halves times 2^14 and the token's weight.
+struct XentError {
+    const int64_t *targets;
+    const float *loss, *lse, *factor;  // factor [M]: 2^14 and the token's weight; 0 without a target
+    uint16_t *out;                     // [M, ld]
+    int64_t ld;
+    int M, N, first;                   // N: columns that exist; those behind them, to the tile's end, become zero
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        const int h4 = 4 * (at.lane >> 5);
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            const int r = at.row(i);
+            const bool row = r < M;
+            const float f = row ? factor[r] : 0.0f;
+            const float base = row ? lse[r] * kLog2e : 0.0f;
+            const int64_t rel = row ? targets[r] - first - at.col0 : -1;
+            const bool here = rel >= 0 && rel < T::WTN;
+            const bool any = __builtin_amdgcn_ballot_w64(here) != 0;
+            const int c = here ? (int)rel - h4 : -1;
+            // exp(-loss) - 1: the target's probability is one less what the others have, to the loss's precision
+            const float e_target = any && here ? f * expm1f(-loss[r]) : 0.0f;
+            const int left = N - at.col0;
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j) {
+                if (at.col0 + 32 * j >= ld) break;
+#pragma unroll
+                for (int g = 0; g < 4; g += 2) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = f * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * g + e], kLog2e, -base));
+                    if (any) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (c == 32 * j + 8 * g + 8 * (e >> 2) + (e & 3)) v[e] = e_target;
+                    }
+                    if (left < T::WTN) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (32 * j + 8 * g + 8 * (e >> 2) + h4 + (e & 3) >= left) v[e] = 0.0f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = f == 0.0f ? 0.0f : v[e];  // (a masked token's lse may be anything)
+                    const u32x4 o = half_pack16(v);
+                    if (row) *reinterpret_cast<u32x4 *>(out + r * ld + at.col0 + 32 * j + 8 * g + 8 * (at.lane >> 5)) = o;
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------------
+// The small kernels.
+// ---------------------------------------------------------------------------------------
+// Joins the sums of a row: eight threads of every row, a block of 32 rows.
+__global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict__ part, const float *__restrict__ z_target,
+                                                        const int64_t *__restrict__ targets, float *__restrict__ loss,
+                                                        float *__restrict__ lse, int M, int N, int parts) {
+    __shared__ f32x2 sh[8][32];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, r = blockIdx.x * 32 + x;
+    auto join = [](f32x2 &t, f32x2 p) {
+        // (an empty part has the base 0 and the sum 0)
+        const float b = p.y == 0.0f ? t.x : t.y == 0.0f ? p.x : __builtin_fmaxf(t.x, p.x);
+        const float s0 = t.y == 0.0f ? 0.0f : t.y * __builtin_amdgcn_exp2f(t.x - b), s1 = p.y == 0.0f ? 0.0f : p.y * __builtin_amdgcn_exp2f(p.x - b);
+        t = f32x2{b, s0 + s1};
+    };
+    f32x2 t = {0.0f, 0.0f};
+    if (r < M) {
+#pragma unroll 4
+        for (int k = y; k < parts; k += 8) join(t, part[(int64_t)k * M + r]);
+    }
+    sh[y][x] = t;
+    __syncthreads();
+    if (y != 0 || r >= M) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) join(t, sh[k][x]);
+    const int64_t target = targets[r];
+    if (target < 0 || target >= N) {
+        lse[r] = (float)(kLn2 * ((double)t.x + log2((double)t.y)));
+        loss[r] = 0.0f;
+    } else {
+        const double z = (double)z_target[r], d = (double)t.x - z * 1.4426950408889634074;
+        // log(1 + sum 2^d)
+        const double l = d < 900.0 ? log1p((double)t.y * exp2(d)) : kLn2 * (d + log2((double)t.y));
+        loss[r] = (float)l;
+        lse[r] = (float)(z + l);
+    }
+}
+
+// A block per row: dst [rows, ld] halves <- src [rows, cols] halves or 8-bit codes, zeros beyond; rows whose target is none are
+// zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).
+template <bool CODES>
+__global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__ src, int64_t ld_src, uint16_t *__restrict__ dst, int64_t ld,
+                                                        int cols, const int64_t *__restrict__ targets, int N) {
+    const int r = blockIdx.x;
+    const bool live = (targets == nullptr || (targets[r] >= 0 && targets[r] < N));
+    for (int c = threadIdx.x * 8; c < ld; c += 256 * 8) {
+        u32x4 o = {0, 0, 0, 0};
+        if (live) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                uint32_t h = 0;
+                if (c + e < cols)
+                    h = CODES ? (uint32_t)((const uint8_t *)src)[r * ld_src + c + e] << 8 : ((const uint16_t *)src)[r * ld_src + c + e];
+                o[e >> 1] |= h << (16 * (e & 1));
+            }
+        }
+        *reinterpret_cast<u32x4 *>(dst + r * ld + c) = o;
+    }
+}
+
+// One block: the exponent of the largest token weight (0 without weights), and every token's factor.
+__global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t *__restrict__ targets, const float *__restrict__ dloss,
+                                                           float *__restrict__ factor, int *__restrict__ exponent, int M, int N) {
+    __shared__ float sh[16];
+    auto live = [&](int r) { return targets[r] >= 0 && targets[r] < N; };
+    int e = 0;
+    if (dloss != nullptr) {
+        float m = 0.0f;
+        for (int r = threadIdx.x; r < M; r += 1024) {
+            const float a = live(r) ? __builtin_fabsf(dloss[r]) : 0.0f;
+            if (a < __builtin_inff()) m = __builtin_fmaxf(m, a);
+        }
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+        if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = m;
+        __syncthreads();
+        m = sh[0];
+#pragma unroll
+        for (int k = 1; k < 16; ++k) m = __builtin_fmaxf(m, sh[k]);
+        // m < 2^e; clamped so that 2^-e is a normal number
+        e = m > 0.0f ? ilogbf(m) + 1 : 0;
+        e = e < -120 ? -120 : e > 120 ? 120 : e;
+    }
+    for (int r = threadIdx.x; r < M; r += 1024)
+        factor[r] = live(r) ? ldexpf(dloss != nullptr ? dloss[r] : 1.0f, kErrorExponent - e) : 0.0f;
+    if (threadIdx.x == 0) *exponent = e;
+}
+
+// out = unscaled sum of `slabs` FP32 matrices [rows, ld]: as halves to nearest, and / or as 8-bit codes.  TR threads per row, four columns
+// each.
+struct XentFinish {
+    const float *sum;
+    int64_t ld, slab;
+    int slabs;
+    const int *exponent;
+    float scale;
+    int64_t rows, cols, row0;  // row0: of the whole output (pieces of dw), for addresses and random bits
+    uint16_t *out16;
+    uint8_t *out8;
+    int sr, sat;
+    uint64_t seed, offset;
+    mp8_stats *stats;
+};
+__global__ __launch_bounds__(256) void xent_finish_kernel(const XentFinish p, int tr) {
+    const float unscale = ldexpf(p.scale, *p.exponent - kErrorExponent);
+    const Philox rng(p.seed, p.offset);
+    StatsAcc st;
+    const uint32_t seen = p.stats != nullptr ? StatsAcc::peek(p.stats) : 0u;
+    const int per = 256 / tr;  // rows of a block
+    const bool whole = (p.cols & 3) == 0;
+    for (int64_t r = (int64_t)blockIdx.x * per + threadIdx.x / tr; r < p.rows; r += (int64_t)gridDim.x * per) {
+        for (int64_t c = 4 * (threadIdx.x % tr); c < p.cols; c += 4 * tr) {
+            f32x4 v = *reinterpret_cast<const f32x4 *>(p.sum + r * p.ld + c);
+            for (int s = 1; s < p.slabs; ++s) v += *reinterpret_cast<const f32x4 *>(p.sum + s * p.slab + r * p.ld + c);
+            const float y[4] = {v.x * unscale, v.y * unscale, v.z * unscale, v.w * unscale};
+            const int64_t at = (p.row0 + r) * p.cols + c;
+            const int n = p.cols - c < 4 ? (int)(p.cols - c) : 4;
+            uint32_t h[4];
+            if (p.out16 != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = f16_from_f32<false>(y[e], 0u);
+                if (whole) {
+                    const u32x2 o = {h[0] | (h[1] << 16), h[2] | (h[3] << 16)};
+                    *reinterpret_cast<u32x2 *>(p.out16 + at) = o;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n) p.out16[at + e] = (uint16_t)h[e];
+                }
+            }
+            if (p.out8 != nullptr) {
+                Words4 w = {0, 0};
+                if (p.sr) w = rng.words_at((uint64_t)at);
+                const uint32_t pk = e5m2_pack4_rt(y, w.r01, w.r23, p.sr != 0, p.sat != 0);
+                if (whole) {
+                    *reinterpret_cast<uint32_t *>(p.out8 + at) = pk;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n) p.out8[at + e] = (uint8_t)(pk >> (8 * e));
+                }
+                if (p.stats != nullptr)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < n) st.add1(y[e], (pk >> (8 * e)) & 0xFFu);
+            } else if (p.stats != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < n) {
+                        if (y[e] != y[e]) st.nan_seen = 1u;
+                        st.amax = __builtin_fmaxf(st.amax, __builtin_fabsf(y[e]));
+                        st.zero_inputs += y[e] == 0.0f ? 1u : 0u;
+                        st.nonfinite += (h[e] & 0x7C00u) == 0x7C00u ? 1u : 0u;
+                        st.zero_codes += (h[e] & 0x7FFFu) == 0u ? 1u : 0u;
+                    }
+            }
+        }
+    }
+    if (p.stats != nullptr) st.flush(p.stats, seen);
+}
+
+// ---------------------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------------------
+namespace {
+
+int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
+
+// Which tiles a product takes, and into how many slices its contraction is cut so that there is a workgroup for
+// every CU.
+struct Plan {
+    int tile;    // 256, 128 or 64
+    int splits;
+};
+Plan plan_tiles(int64_t rows, int64_t cols, int64_t kc, bool may_split) {
+    auto tiles = [&](int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); };
+    Plan p{64, 1};
+    if (tiles(256) >= 192) p.tile = 256;
+    else if (tiles(128) >= 192) p.tile = 128;
+    if (may_split && p.tile == 64) {
+        const int64_t steps = (kc + 63) / 64, want = 512 / tiles(64);
+        int64_t s = steps / 4 < want ? steps / 4 : want;
+        p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+    }
+    return p;
+}
+
+struct Shape {
+    int64_t M, N, K, Kp;
+    bool copy_x, copy_w;
+    int64_t piece;  // classes per piece
+};
+
+constexpr int64_t kPieceBytes = (int64_t)512 << 20;
+
+bool aligned_ld(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0; }
+
+Shape make_shape(int64_t M, int64_t N, int64_t K, bool copy_x, bool copy_w, bool backward) {
+    Shape s{M, N, K, up(K, 64), copy_x, copy_w, N};
+    // bytes per class: of e and of the FP32 sums of dw, of a copy of w
+    const int64_t row_e = backward ? (2 * M > 4 * s.Kp ? 2 * M : 4 * s.Kp) : 0, row_w = copy_w ? 2 * s.Kp : 0, row = row_e > row_w ? row_e : row_w;
+    if (row) {
+        int64_t n = kPieceBytes / row / 256 * 256;
+        n = n < 2048 ? 2048 : n;
+        const int64_t pieces = (N + n - 1) / n;
+        s.piece = pieces == 1 ? N : up((N + pieces - 1) / pieces, 256);
+    }
+    return s;
+}
+
+// The workspace, in order; every part starts at a multiple of 256 bytes.
+struct Layout {
+    size_t x, w, part, z_target;             // forward: copies of x and of a piece of w, the sums, the targets' logits
+    size_t factor, exponent, e, dx, dw, total;  // backward: (copies as above,) the tokens' factors, e, FP32 sums
+};
+int parts_of(const Shape &s) {  // sums per token
+    int n = 0;
+    for (int64_t c = 0; c < s.N; c += s.piece) {
+        const int64_t cols = s.N - c < s.piece ? s.N - c : s.piece;
+        const int w = plan_tiles(s.M, cols, s.K, false).tile / 2;
+        n += (int)((cols + w - 1) / w);
+    }
+    return n;
+}
+struct BwdPlans {
+    Plan dx, dw;
+};
+BwdPlans bwd_plans(const Shape &s) {
+    const int64_t n = s.piece < s.N ? s.piece : s.N;
+    return {plan_tiles(s.M, s.K, n, true), plan_tiles(n, s.K, s.M, true)};
+}
+Layout make_layout(const Shape &s, bool backward, bool dx, bool dw) {
+    Layout l{};
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t here = at;
+        at += (size_t)up(bytes, 256);
+        return here;
+    };
+    if (s.copy_x) l.x = take(2 * s.M * s.Kp);
+    if (s.copy_w) l.w = take(2 * up(s.piece, 8) * s.Kp);
+    if (!backward) {
+        l.part = take(8 * (int64_t)parts_of(s) * s.M);
+        l.z_target = take(4 * s.M);
+    } else {
+        l.factor = take(4 * s.M);
+        l.exponent = take(4);
+        l.e = take(2 * s.M * up(s.piece, 64));
+        const BwdPlans p = bwd_plans(s);
+        if (dx) l.dx = take(4 * p.dx.splits * s.M * s.Kp);
+        if (dw) l.dw = take(4 * p.dw.splits * s.piece * s.Kp);
+    }
+    l.total = at;
+    return l;
+}
+
+// Sizes every product of which fits 63 bits and every 32-bit offset of a kernel: a tile's rows span 256 * ld * 2 bytes.
+mp8_status check_sizes(int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw) {
+    if (M < 0 || N < 0 || K < 0) return MP8_ERR_INVALID_ARG;
+    const int64_t most = (int64_t)1 << 22;
+    if (M > most || N > most || K > ((int64_t)1 << 20)) return MP8_ERR_UNSUPPORTED;
+    if (((M + 255) / 256) * ((N + 255) / 256) > ((int64_t)1 << 23)) return MP8_ERR_UNSUPPORTED;  // workgroups of a launch
+    if (ldx < K || ldw < K) return MP8_ERR_INVALID_ARG;
+    if (ldx > ((int64_t)1 << 21) || ldw > ((int64_t)1 << 21)) return MP8_ERR_UNSUPPORTED;
+    return MP8_OK;
+}
+
+template <bool BTN, bool ATN, class Epi>
+bool product(int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t cols, int64_t kc, int splits,
+             const Epi &epi, hipStream_t stream) {
+    const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows, cols, kc, tile, tile, splits, false);
+    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, 1, epi, stream);
+    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, 1, epi, stream);
+    return half_gemm_launch<Half64, ATN, BTN>(p, 1, epi, stream);
+}
+
+bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t ld, int64_t rows, int64_t cols,
+               const int64_t *targets, int64_t N, hipStream_t stream) {
+    if (codes)
+        hipLaunchKernelGGL((xent_copy_kernel<true>), dim3((unsigned)rows), dim3(256), 0, stream, src, ld_src, dst, ld, (int)cols, targets, (int)N);
+    else
+        hipLaunchKernelGGL((xent_copy_kernel<false>), dim3((unsigned)rows), dim3(256), 0, stream, src, ld_src, dst, ld, (int)cols, targets, (int)N);
+    return hipGetLastError() == hipSuccess;
+}
+
+}  // namespace
+}  // namespace mp8
+
+extern "C" size_t mp8_softmax_xent_fwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t ldw) {
+    using namespace mp8;
+    if (check_sizes(M, N, K, K, ldw) != MP8_OK || M == 0 || N == 0 || K == 0) return 0;
+    return make_layout(make_shape(M, N, K, true, !aligned_ld(K, ldw), false), false, false, false).total;
+}
+
+extern "C" size_t mp8_softmax_xent_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t ldw) {
+    using namespace mp8;
+    if (check_sizes(M, N, K, K, ldw) != MP8_OK || M == 0 || N == 0 || K == 0) return 0;
+    return make_layout(make_shape(M, N, K, true, !aligned_ld(K, ldw), true), true, true, true).total;
+}
+
+extern "C" mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K, const void *x, int x_is_e5m2, int64_t ldx,
+                                                const uint16_t *w, int64_t ldw, const int64_t *targets, float *loss, float *lse,
+                                                void *workspace, size_t workspace_bytes, void *stream) {
+    using namespace mp8;
+    const mp8_status sizes = check_sizes(M, N, K, ldx, ldw);
+    if (sizes != MP8_OK) return sizes;
+    if (M == 0 || N == 0 || K == 0) return MP8_OK;
+    if (!x || !w || !targets || !loss || !lse) return MP8_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)workspace) & 15u) return MP8_ERR_ALIGNMENT;
+    const Shape s = make_shape(M, N, K, x_is_e5m2 || !aligned_ld(K, ldx), !aligned_ld(K, ldw), false);
+    const Layout l = make_layout(s, false, false, false);
+    if (!workspace || workspace_bytes < l.total) return MP8_ERR_WORKSPACE;
+    uint8_t *ws = (uint8_t *)workspace;
+    hipStream_t st = (hipStream_t)stream;
+    const uint16_t *xs = (const uint16_t *)x;
+    int64_t ld_x = ldx;
+    if (s.copy_x) {
+        xs = (uint16_t *)(ws + l.x);
+        if (!copy_half(x, x_is_e5m2 != 0, ldx, (uint16_t *)(ws + l.x), s.Kp, M, K, nullptr, N, st)) return MP8_ERR_HIP;
+        ld_x = s.Kp;
+    }
+    int parts = 0;
+    for (int64_t c = 0; c < N; c += s.piece) {
+        const int64_t cols = N - c < s.piece ? N - c : s.piece;
+        const uint16_t *wp = w + c * ldw;
+        int64_t ld_w = ldw;
+        if (s.copy_w) {
+            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, st)) return MP8_ERR_HIP;
+            wp = (uint16_t *)(ws + l.w);
+            ld_w = s.Kp;
+        }
+        const int tile = plan_tiles(M, cols, K, false).tile;
+        const XentStats epi{targets, (f32x2 *)(ws + l.part), (float *)(ws + l.z_target), (int)M, (int)cols, (int)c, parts};
+        if (!product<false, false>(tile, xs, ld_x, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        parts += (int)((cols + tile / 2 - 1) / (tile / 2));
+    }
+    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(256), 0, st, (const f32x2 *)(ws + l.part), (const float *)(ws + l.z_target),
+                       targets, loss, lse, (int)M, (int)N, parts);
+    return hipGetLastError() == hipSuccess ? MP8_OK : MP8_ERR_HIP;
+}
+
+extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K, const void *x, int x_is_e5m2, int64_t ldx,
+                                                const uint16_t *w, int64_t ldw, const int64_t *targets, const float *loss,
+                                                const float *lse, const float *dloss, float scale, uint16_t *dx16, uint8_t *dx8,
+                                                uint16_t *dw16, uint8_t *dw8, mp8_round round, int flags, uint64_t seed,
+                                                uint64_t dx_offset, uint64_t dw_offset, mp8_stats *dx_stats, mp8_stats *dw_stats,
+                                                void *workspace, size_t workspace_bytes, void *stream) {
+    using namespace mp8;
+    const mp8_status sizes = check_sizes(M, N, K, ldx, ldw);
+    if (sizes != MP8_OK) return sizes;
+    if (round != MP8_RNE && round != MP8_SR) return MP8_ERR_INVALID_ARG;
+    if (flags & ~MP8_FLAG_SATURATE) return MP8_ERR_INVALID_ARG;
+    if (M == 0 || N == 0 || K == 0) return MP8_OK;
+    const bool dx = dx16 || dx8, dw = dw16 || dw8;
+    if (!dx && !dw) return MP8_ERR_INVALID_ARG;
+    if (!x || !w || !targets || !loss || !lse) return MP8_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx16 | (uintptr_t)dx8 | (uintptr_t)dw16 | (uintptr_t)dw8 | (uintptr_t)workspace) & 15u)
+        return MP8_ERR_ALIGNMENT;
+    const Shape s = make_shape(M, N, K, true, !aligned_ld(K, ldw), true);
+    const Layout l = make_layout(s, true, dx, dw);
+    if (!workspace || workspace_bytes < l.total) return MP8_ERR_WORKSPACE;
+    uint8_t *ws = (uint8_t *)workspace;
+    hipStream_t st = (hipStream_t)stream;
+    uint16_t *xs = (uint16_t *)(ws + l.x), *e = (uint16_t *)(ws + l.e);
+    float *factor = (float *)(ws + l.factor), *dxs = (float *)(ws + l.dx), *dws = (float *)(ws + l.dw);
+    int *exponent = (int *)(ws + l.exponent);
+    if (!copy_half(x, x_is_e5m2 != 0, ldx, xs, s.Kp, M, K, targets, N, st)) return MP8_ERR_HIP;
+    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, dloss, factor, exponent, (int)M, (int)N);
+    if (hipGetLastError() != hipSuccess) return MP8_ERR_HIP;
+    const int64_t K8 = up(K, 8), lde = up(s.piece, 64);
+    const BwdPlans plans = bwd_plans(s);
+    auto finish = [&](const float *sum, int64_t slab, int slabs, int64_t rows, int64_t row0, uint16_t *out16, uint8_t *out8, uint64_t offset,
+                      mp8_stats *stats) {
+        const XentFinish f{sum, s.Kp, slab, slabs, exponent, scale, rows, K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0,
+                           seed, offset, stats};
+        int tr = 1;
+        while (tr < 256 && 4 * tr < K) tr *= 2;
+        int64_t blocks = (rows + 256 / tr - 1) / (256 / tr);
+        if (stats != nullptr && blocks > 2048) blocks = 2048;
+        hipLaunchKernelGGL(xent_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f, tr);
+        return hipGetLastError() == hipSuccess;
+    };
+    for (int64_t c = 0; c < N; c += s.piece) {
+        const int64_t cols = N - c < s.piece ? N - c : s.piece;
+        const uint16_t *wp = w + c * ldw;
+        int64_t ld_w = ldw;
+        if (s.copy_w) {
+            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, st)) return MP8_ERR_HIP;
+            wp = (uint16_t *)(ws + l.w);
+            ld_w = s.Kp;
+        }
+        const XentError epi{targets, loss, lse, factor, e, lde, (int)M, (int)cols, (int)c};
+        if (!product<false, false>(plan_tiles(M, cols, K, false).tile, xs, s.Kp, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        if (dx) {
+            const HalfEpiSum sum{dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
+            if (!product<true, false>(plans.dx.tile, e, lde, wp, ld_w, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
+        }
+        if (dw) {
+            const HalfEpiSum sum{dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
+            if (!product<true, true>(plans.dw.tile, e, lde, xs, s.Kp, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
+            if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
+        }
+    }
+    if (dx && !finish(dxs, M * s.Kp, plans.dx.splits, M, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
+    return MP8_OK;
+}
