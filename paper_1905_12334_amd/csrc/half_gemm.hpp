@@ -67,16 +67,17 @@ __device__ __forceinline__ HalfTile half_tile(const HalfGemm &p) {
     return t;
 }
 
-// Tiles: four waves, WGM x WGN of them, each with a grid of 32x32 accumulators.
-template <int BM_, int BN_, int NSTAGE_, int MINBLOCKS_>
+// Tiles: four waves, WGM x WGN of them, each with a grid of 32x32 accumulators.  WHOLE: how far ahead fragments are fetched, see the kernel.
+template <int BM_, int BN_, int NSTAGE_, int MINBLOCKS_, bool WHOLE_>
 struct HalfTiling {
     static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = 2, NSTAGE = NSTAGE_, MINBLOCKS = MINBLOCKS_;
     static constexpr int WTM = BM / WGM, WTN = BN / WGN, MT = WTM / 32, NT = WTN / 32;
+    static constexpr bool WHOLE = WHOLE_;
 };
+using Half256 = HalfTiling<256, 256, 2, 1, false>;
+using Half128 = HalfTiling<128, 128, 2, 2, true>;
+using Half64 = HalfTiling<64, 64, 4, 2, true>;
 using f32x2 = float __attribute__((ext_vector_type(2)));
-using Half256 = HalfTiling<256, 256, 2, 1>;
-using Half128 = HalfTiling<128, 128, 2, 2>;
-using Half64 = HalfTiling<64, 64, 4, 2>;
 
 // Where a lane's accumulators lie.  Element e of accumulator (i, j) is row row(i), column col(j) + 8 (e / 4) + e % 4.
 template <class T>
@@ -88,10 +89,18 @@ struct HalfPlace {
     __device__ __forceinline__ int col(int j) const { return col0 + 32 * j + 4 * (lane >> 5); }
 };
 
-// The pipeline is the one of gemm_mfma_kernel (a ring of 128-byte-wide operand slabs in LDS, direct-to-LDS loads, one barrier per
-// stage, fragments fetched one sub-step ahead, everything between two matrix instructions), with four sub-steps of sixteen
-// contraction indices per stage: the barrier stands behind the third, by which all fragments of the stage have
-// been read.  Slab images:
+// Operands pass through a ring of 128-byte-wide slabs in LDS, filled by direct-to-LDS loads, a stage (64 contraction indices)
+// being four sub-steps of sixteen.  Two schedules:
+//   one wave per SIMD (256x256): as in gemm_mfma_kernel, fragments are fetched one sub-step ahead, everything stands between two
+//     matrix instructions, and the barrier stands behind the third sub-step, by which all fragments of the stage have been read
+//   WHOLE (two workgroups per CU): behind the barrier all fragments of the next stage are requested, then the loads of the stage that
+//     takes the place of the current one, then the current stage is multiplied; the other workgroup fills what is left
+// Gaussian operands, contraction 4096, TFLOP/s: 4096 x 4096 in 256x256 tiles 1090, in 128x128 tiles 1015 (with the other schedule 915), in
+// 64x64 tiles 570.  What bounds them: the 256x256 tile the power such data draws (all ones: 1390) and the clock it leaves
+// (1.85 GHz, 59 % of the cycles with a matrix instruction; loads that always hit, 1550), the small ones what a CU gets from L2 (14 TB/s in
+// all).  A row pitch that is a multiple of some KB costs up to 15 % (8192 x 2048 x 32768, pitch 64 KB 938, 128 bytes more 1105):
+// matrices laid out here have an odd number of 128-byte lines per row (half_pitch).
+// Slab images:
 //   row-major: row r is 128 bytes, its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7)
 //   contraction-major: panels of 64 tile rows; 64 contraction rows of 128 bytes, chunk c of contraction row k in slot
 //     c ^ (4 ((k >> 1) & 1)).  The transposing read names 4 x 4 halves per 16 lanes: lanes 0 .. 31 read four contraction
@@ -184,14 +193,17 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
-    auto wait_stage = [&](int s) {  // stage s has landed; later ones may be under way
-        int later = ks_count - 1 - s;
-        later = later < NSTAGE - 2 ? later : NSTAGE - 2;
-        if (NSTAGE > 2 && later >= NSTAGE - 2) wait_vm_lds<G * (NSTAGE - 2)>();
-        else if (NSTAGE > 3 && later == 1) wait_vm_lds<G>();
+    // at most `later` (0 .. NSTAGE - 1) whole stages of this wave's loads under way
+    auto wait_later = [&](int later) {
+        if (later >= NSTAGE - 1) wait_vm_lds<G * (NSTAGE - 1)>();
+        else if (later == NSTAGE - 2) wait_vm_lds<G * (NSTAGE - 2)>();
+        else if (NSTAGE == 4 && later == 1) wait_vm_lds<NSTAGE == 4 ? G : 0>();
         else wait_vm_lds<0>();
     };
-    half8 fr[2][F];
+    auto wait_stage = [&](int s) {  // stage s has landed; the buffer of stage s - 1 has not been given away yet
+        const int later = ks_count - 1 - s;
+        wait_later(later < NSTAGE - 2 ? later : NSTAGE - 2);
+    };
 #pragma unroll
     for (int s = 0; s < NSTAGE; ++s)
         if (s < ks_count) {
@@ -200,40 +212,72 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
                 for (int q = 0; q < G; ++q) issue_one(s, q);
         }
-    // (the whole ring has been issued: up to NSTAGE - 1 stages lie behind the first)
-    if (ks_count >= NSTAGE) wait_vm_lds<G * (NSTAGE - 1)>();
-    else if (NSTAGE > 3 && ks_count == 3) wait_vm_lds<2 * G>();
-    else if (NSTAGE > 2 && ks_count == 2) wait_vm_lds<G>();
-    else wait_vm_lds<0>();
+    wait_later((ks_count < NSTAGE ? ks_count : NSTAGE) - 1);
     __syncthreads();
+    if constexpr (T::WHOLE) {
+        half8 fr[2][4][F];
+        auto read = [&](int s, half8 (&to)[4][F]) {
 #pragma unroll
-    for (int n = 0; n < F; ++n) fr[0][order(n)] = fragment(0, 0, order(n));
-    constexpr int R = (F + NM - 1) / NM, D = (G + NM - 1) / NM;  // fragment reads and loads per matrix instruction
-    for (int t = 0; t < ks_count; ++t) {
-        const bool more = t + NSTAGE < ks_count, next = t + 1 < ks_count;
+            for (int sub = 0; sub < 4; ++sub)
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) {
+                for (int n = 0; n < F; ++n) to[sub][order(n)] = fragment(s, sub, order(n));
+        };
+        auto stage = [&](int t, half8 (&now)[4][F], half8 (&then)[4][F]) {
+            if (t + 1 < ks_count) {
+                wait_stage(t + 1);
+                __syncthreads();  // the fragments of stage t have been read everywhere
+                read(t + 1, then);
+                if (t + NSTAGE < ks_count) {
 #pragma unroll
-            for (int k = 0; k < NM; ++k) {
-                const int i = k / NT, j = k % NT;
-                // b goes in as the "row" matrix so that a lane ends up with consecutive output columns
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[sub & 1][MT + j], fr[sub & 1][i], acc[i][j], 0, 0, 0);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int n = k * R + r;
-                    if (n < F && (sub < 3 || next)) fr[(sub + 1) & 1][order(n)] = fragment(sub < 3 ? t : t + 1, (sub + 1) & 3, order(n));
+                    for (int q = 0; q < G; ++q) issue_one(t + NSTAGE, q);
                 }
-                if (sub == 3 && more) {
-#pragma unroll
-                    for (int r = 0; r < D; ++r)
-                        if (k * D + r < G) issue_one(t + NSTAGE, k * D + r);
-                }
-                __builtin_amdgcn_sched_barrier(0);
             }
-            if (sub == 2) {
-                if (next) wait_stage(t + 1);
-                else wait_vm_lds<63>();
-                __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub)
+#pragma unroll
+                for (int k = 0; k < NM; ++k)
+                    acc[k / NT][k % NT] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[sub][MT + k % NT], now[sub][k / NT], acc[k / NT][k % NT], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        read(0, fr[0]);
+        int t = 0;
+        for (; t + 1 < ks_count; t += 2) {
+            stage(t, fr[0], fr[1]);
+            stage(t + 1, fr[1], fr[0]);
+        }
+        if (t < ks_count) stage(t, fr[0], fr[1]);
+    } else {
+        half8 fr[2][F];
+#pragma unroll
+        for (int n = 0; n < F; ++n) fr[0][order(n)] = fragment(0, 0, order(n));
+        constexpr int R = (F + NM - 1) / NM, D = (G + NM - 1) / NM;  // fragment reads and loads per matrix instruction
+        for (int t = 0; t < ks_count; ++t) {
+            const bool more = t + NSTAGE < ks_count, next = t + 1 < ks_count;
+#pragma unroll
+            for (int sub = 0; sub < 4; ++sub) {
+#pragma unroll
+                for (int k = 0; k < NM; ++k) {
+                    const int i = k / NT, j = k % NT;
+                    // b goes in as the "row" matrix so that a lane ends up with consecutive output columns
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fr[sub & 1][MT + j], fr[sub & 1][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const int n = k * R + r;
+                        if (n < F && (sub < 3 || next)) fr[(sub + 1) & 1][order(n)] = fragment(sub < 3 ? t : t + 1, (sub + 1) & 3, order(n));
+                    }
+                    if (sub == 3 && more) {
+#pragma unroll
+                        for (int r = 0; r < D; ++r)
+                            if (k * D + r < G) issue_one(t + NSTAGE, k * D + r);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (sub == 2) {
+                    if (next) wait_stage(t + 1);
+                    else wait_vm_lds<63>();
+                    __syncthreads();
+                }
             }
         }
     }
@@ -246,10 +290,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 __device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
     uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const half2v h = {(_Float16)v[2 * q], (_Float16)v[2 * q + 1]};
-        w[q] = __builtin_bit_cast(uint32_t, h);
-    }
+    for (int q = 0; q < 4; ++q) w[q] = f16_from_f32<false>(v[2 * q], 0u) | f16_from_f32<false>(v[2 * q + 1], 0u) << 16;
     const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
     const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     return u32x4{s0[0], s1[0], s0[1], s1[1]};
@@ -294,7 +335,49 @@ struct HalfEpiSum {
     }
 };
 
-// Host side: the geometry of a call.  Sizes have been checked: rows, cols, kc >= 1 and what HalfGemm says.
+// ---------------------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------------------
+// Row pitch in halves of a matrix that is laid out here: whole 128-byte lines, an odd number of them.
+static inline int64_t half_pitch(int64_t n) { return ((n + 63) / 64 | 1) * 64; }
+
+// Which tiles a product takes and into how many slices its contraction is cut.
+struct HalfPlan {
+    int tile, splits;
+};
+
+// Estimated time, us, of `tiles` tiles over `stages` stages.  Measured (4096 x 4096 x 4096 and parts of it), us per stage: 64x64 tiles, up to 256
+// of them 0.25, up to 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93; 256x256, 128 1.36, 256 1.73; more tiles take rounds.  On top
+// come start and end of a workgroup.
+static inline double half_cost(int tile, int64_t tiles, double stages) {
+    const int64_t slots = tile == 256 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
+    const double whole = tile == 256 ? 1.73 : tile == 128 ? 0.93 : 0.41, half = tile == 256 ? 1.36 : tile == 128 ? 0.69 : 0.25;
+    const double base = tile == 256 ? 10.0 : tile == 128 ? 5.0 : 3.5;
+    const double rounds = (double)(full + (rest != 0));
+    return base * (rounds < 1 ? 1 : 0.5 + 0.5 * rounds) + stages * ((double)full * whole + (rest == 0 ? 0.0 : rest <= slots / 2 ? half : whole));
+}
+
+// most_splits > 1: the slices' FP32 sums are written and added up by a pass of its own.
+static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int64_t kc, bool symmetric, int most_splits) {
+    HalfPlan best{64, 1};
+    double least = 1e300;
+    for (const int tile : {256, 128, 64}) {
+        const int64_t tm = (rows + tile - 1) / tile, tn = (cols + tile - 1) / tile;
+        const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn), steps = (kc + 63) / 64;
+        if (tiles > (int64_t)1 << 23) continue;
+        for (int s = 1; s <= most_splits && s <= steps; s = s < 8 ? s + 1 : s + s / 4) {
+            // (slices of one more pass: 4 bytes out and in again per element and slice, at 4 TB/s)
+            const double t = half_cost(tile, tiles * s, (double)((steps + s - 1) / s)) + (s > 1 ? 2.0e-6 * (double)(batch * rows * cols) * s : 0.0);
+            if (t < least) {
+                least = t;
+                best = {tile, s};
+            }
+        }
+    }
+    return best;
+}
+
+// The geometry of a call.  Sizes have been checked: rows, cols, kc >= 1 and what HalfGemm says.
 static inline HalfGemm half_gemm_args(const void *a, int64_t lda, int64_t a_batch, const void *b, int64_t ldb, int64_t b_batch, int64_t rows,
                                       int64_t cols, int64_t kc, int tile_m, int tile_n, int splits, bool symmetric) {
     HalfGemm p{};

@@ -317,8 +317,8 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     l.n = rows < cols ? cols : rows;
     l.m8 = up(l.m, 8);
     l.n8 = up(l.n, 8);
-    l.ld = up(l.n, 64);
-    l.lda = up(l.m, 64);
+    l.ld = half_pitch(l.n);
+    l.lda = half_pitch(l.m);
     const int64_t want = (rows * cols + 4095) / 4096, most = batch >= 256 ? 4 : 1024 / batch;
     l.blocks = (int)(want < 1 ? 1 : want > most ? most : want);
     size_t at = 0;
@@ -347,19 +347,10 @@ mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
     return MP8_OK;
 }
 
-// The largest tile that still gives most CUs one.
-int ortho_tile(int64_t batch, int64_t rows, int64_t cols, bool symmetric) {
-    auto tiles = [&](int64_t t) {
-        const int64_t a = (rows + t - 1) / t, b = (cols + t - 1) / t;
-        return batch * (symmetric ? a * (a + 1) / 2 : a * b);
-    };
-    return tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : 64;
-}
-
 template <bool BTN, class Epi>
 bool ortho_product(int64_t batch, const uint16_t *a, int64_t lda, int64_t a_batch, const uint16_t *b, int64_t ldb, int64_t b_batch, int64_t rows,
                    int64_t cols, int64_t kc, bool symmetric, const uint32_t *skip, const Epi &epi, hipStream_t stream) {
-    const int tile = ortho_tile(batch, rows, cols, symmetric);
+    const int tile = half_plan(batch, rows, cols, kc, symmetric, 1).tile;
     HalfGemm p = half_gemm_args(a, lda, a_batch, b, ldb, b_batch, rows, cols, kc, tile, tile, 1, symmetric);
     p.skip = skip;
     if (tile == 256) return half_gemm_launch<Half256, false, BTN>(p, batch, epi, stream);

@@ -26,17 +26,24 @@ constexpr int kErrorExponent = 14;
 // Sums are of powers of two: with base B = fl(m log2 e), sum 2^(z log2 e - B), one rounding per exponent (a fused multiply-add);
 // what B itself was rounded by cancels when the sums are joined.  The target's logit is kept apart: the loss is
 // log(1 + what the others have beside it), which lse - z would not give where the target has nearly everything.
+// An empty part has the base 0 and the sum 0.
+__device__ __forceinline__ void xent_join(f32x2 &t, f32x2 p) {
+    const float b = p.y == 0.0f ? t.x : t.y == 0.0f ? p.x : __builtin_fmaxf(t.x, p.x);
+    const float s0 = t.y == 0.0f ? 0.0f : t.y * __builtin_amdgcn_exp2f(t.x - b), s1 = p.y == 0.0f ? 0.0f : p.y * __builtin_amdgcn_exp2f(p.x - b);
+    t = f32x2{b, s0 + s1};
+}
+
 struct XentStats {
     const int64_t *targets;
-    f32x2 *part;     // [parts, M]: (B, sum) of the columns of one wave's tile, without the target
+    f32x2 *part;     // [parts, M]: (B, sum) of the columns of one tile, without the target
     float *z_target; // [M]
     int M, N, first; // `first`: class of this piece's column 0
     int part0;       // of this piece
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
         const int h4 = 4 * (at.lane >> 5), left = N - at.col0;  // columns of this wave's tile that exist
-        if (left <= 0) return;
         int64_t target[T::MT];
+        f32x2 mine[T::MT];
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) target[i] = at.row(i) < M ? targets[at.row(i)] : -1;
 #pragma unroll
@@ -77,8 +84,22 @@ struct XentStats {
                 for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base));
             const auto sums = __builtin_amdgcn_permlane32_swap(f2u(s), f2u(s), false, false);
             s = u2f(sums[0]) + u2f(sums[1]);
-            const int r = at.row(i);
-            if (at.lane < 32 && r < M) part[(int64_t)(part0 + at.col0 / T::WTN) * M + r] = f32x2{base, s};
+            mine[i] = f32x2{base, s};
+        }
+        // the right-hand waves hand over to the left-hand ones
+        __shared__ f32x2 right[T::BM];
+        const int wm = at.wave / T::WGN, wn = at.wave % T::WGN;
+        if (wn == 1 && at.lane < 32) {
+#pragma unroll
+            for (int i = 0; i < T::MT; ++i) right[wm * T::WTM + 32 * i + at.lane] = mine[i];
+        }
+        __syncthreads();
+        if (wn == 0 && at.lane < 32) {
+#pragma unroll
+            for (int i = 0; i < T::MT; ++i) {
+                xent_join(mine[i], right[wm * T::WTM + 32 * i + at.lane]);
+                if (at.row(i) < M) part[(int64_t)(part0 + at.tn) * M + at.row(i)] = mine[i];
+            }
         }
     }
 };
@@ -134,31 +155,111 @@ struct XentError {
     }
 };
 
+// Statistics of a value that is stored as a half.
+__device__ __forceinline__ void xent_count_half(StatsAcc &st, float y) {
+    const uint32_t h = f16_from_f32<false>(y, 0u);
+    if (y != y) st.nan_seen = 1u;
+    st.amax = __builtin_fmaxf(st.amax, __builtin_fabsf(y));
+    st.zero_inputs += y == 0.0f ? 1u : 0u;
+    st.nonfinite += (h & 0x7C00u) == 0x7C00u ? 1u : 0u;
+    st.zero_codes += (h & 0x7FFFu) == 0u ? 1u : 0u;
+}
+
+// A gradient, complete in its tile: unscaled, rounded and stored.  Rows of whole groups of eight.  FULL: with codes and statistics, which
+// take more code and registers than fit beside the accumulators of a 256x256 tile (they went to memory: 8192 x 131072 x 2048 six
+// times as long); its callers take 128x128 tiles then.
+template <bool FULL>
+struct XentOut {
+    const int *exponent;
+    float scale;
+    int rows, cols;
+    int64_t row0;  // of the whole output (pieces of dw), for addresses and random bits
+    uint16_t *out16;
+    uint8_t *out8;
+    int sr, sat;
+    uint64_t seed, offset;
+    mp8_stats *stats;
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        const float unscale = ldexpf(scale, *exponent - kErrorExponent);
+        const Philox rng(seed, offset);
+        StatsAcc st;
+        const uint32_t seen = FULL && stats != nullptr ? StatsAcc::peek(stats) : 0u;
+        const int h = at.lane >> 5;
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            const int r = at.row(i);
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j) {
+                if (at.col0 + 32 * j >= cols) break;
+#pragma unroll
+                for (int g = 0; g < 4; g += 2) {
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = acc[i][j][4 * g + e] * unscale;
+                    // before the half waves exchange: columns 8 g + 4 h .. and eight further; after it: eight from 8 (g + h) on
+                    const int c = at.col0 + 32 * j + 8 * g, mine = c + 8 * h;
+                    const int64_t first = (row0 + r) * (int64_t)cols + c;
+                    const bool in0 = r < rows && c < cols, in1 = r < rows && c + 8 < cols, in = h ? in1 : in0;
+                    if (!FULL || out16 != nullptr) {
+                        const u32x4 o = half_pack16(v);
+                        if (in) *reinterpret_cast<u32x4 *>(out16 + first + mine - c) = o;
+                    }
+                    if (FULL && out8 != nullptr) {
+                        Words4 w0 = {0, 0}, w1 = {0, 0};
+                        if (sr) {  // each half wave makes one of the two blocks and hands over the half it does not need
+                            const uint4 b = rng.block((uint64_t)(first + 8 * h) >> 3);
+                            const auto s01 = __builtin_amdgcn_permlane32_swap(b.x, b.z, false, false);
+                            const auto s23 = __builtin_amdgcn_permlane32_swap(b.y, b.w, false, false);
+                            w0 = {s01[0], s23[0]};
+                            w1 = {s01[1], s23[1]};
+                        }
+                        const uint32_t p0 = e5m2_pack4_rt(v, w0.r01, w0.r23, sr != 0, sat != 0), p1 = e5m2_pack4_rt(v + 4, w1.r01, w1.r23, sr != 0, sat != 0);
+                        if (stats != nullptr) {
+                            if (in0) st.add4(v, p0);
+                            if (in1) st.add4(v + 4, p1);
+                        }
+                        const auto s = __builtin_amdgcn_permlane32_swap(p0, p1, false, false);
+                        const u32x2 o = {s[0], s[1]};
+                        if (in) *reinterpret_cast<u32x2 *>(out8 + first + mine - c) = o;
+                    } else if (FULL && stats != nullptr) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (e < 4 ? in0 : in1) xent_count_half(st, v[e]);
+                    }
+                }
+            }
+        }
+        if (FULL && stats != nullptr) st.flush(stats, seen);
+    }
+};
+
 // ---------------------------------------------------------------------------------------
 // The small kernels.
 // ---------------------------------------------------------------------------------------
-// Joins the sums of a row: eight threads of every row, a block of 32 rows.
+// Joins the sums of a row: R rows per block, 256 / R threads each.
+template <int R>
 __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict__ part, const float *__restrict__ z_target,
                                                         const int64_t *__restrict__ targets, float *__restrict__ loss,
                                                         float *__restrict__ lse, int M, int N, int parts) {
-    __shared__ f32x2 sh[8][32];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, r = blockIdx.x * 32 + x;
-    auto join = [](f32x2 &t, f32x2 p) {
-        // (an empty part has the base 0 and the sum 0)
-        const float b = p.y == 0.0f ? t.x : t.y == 0.0f ? p.x : __builtin_fmaxf(t.x, p.x);
-        const float s0 = t.y == 0.0f ? 0.0f : t.y * __builtin_amdgcn_exp2f(t.x - b), s1 = p.y == 0.0f ? 0.0f : p.y * __builtin_amdgcn_exp2f(p.x - b);
-        t = f32x2{b, s0 + s1};
-    };
+    constexpr int Y = 256 / R;
+    __shared__ f32x2 sh[Y][R];
+    const int x = threadIdx.x % R, y = threadIdx.x / R, r = blockIdx.x * R + x;
     f32x2 t = {0.0f, 0.0f};
     if (r < M) {
 #pragma unroll 4
-        for (int k = y; k < parts; k += 8) join(t, part[(int64_t)k * M + r]);
+        for (int k = y; k < parts; k += Y) xent_join(t, part[(int64_t)k * M + r]);
     }
     sh[y][x] = t;
-    __syncthreads();
-    if (y != 0 || r >= M) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) join(t, sh[k][x]);
+    for (int h = Y / 2; h; h /= 2) {
+        __syncthreads();
+        if (y < h) {
+            xent_join(t, sh[y + h][x]);
+            sh[y][x] = t;
+        }
+    }
+    if (y != 0 || r >= M) return;
     const int64_t target = targets[r];
     if (target < 0 || target >= N) {
         lse[r] = (float)(kLn2 * ((double)t.x + log2((double)t.y)));
@@ -172,22 +273,41 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
     }
 }
 
-// A block per row: dst [rows, ld] halves <- src [rows, cols] halves or 8-bit codes, zeros beyond; rows whose target is none are
-// zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).
-template <bool CODES>
+// dst [rows, ld] halves <- src [rows, cols] halves or 8-bit codes, zeros beyond, TR threads per row; rows whose target is none are
+// zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).  VEC: rows of
+// whole, aligned groups of eight.  factor, where given, becomes that of a call without token weights.
+template <bool CODES, bool VEC>
 __global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__ src, int64_t ld_src, uint16_t *__restrict__ dst, int64_t ld,
-                                                        int cols, const int64_t *__restrict__ targets, int N) {
-    const int r = blockIdx.x;
-    const bool live = (targets == nullptr || (targets[r] >= 0 && targets[r] < N));
-    for (int c = threadIdx.x * 8; c < ld; c += 256 * 8) {
+                                                        int rows, int cols, const int64_t *__restrict__ targets, int N, int tr,
+                                                        float *__restrict__ factor, int *__restrict__ exponent) {
+    const int64_t r = (int64_t)blockIdx.x * (256 / tr) + threadIdx.x / tr;
+    const int c0 = 8 * (threadIdx.x % tr);
+    if (r >= rows) return;
+    const bool live = targets == nullptr || (targets[r] >= 0 && targets[r] < N);
+    if (factor != nullptr && c0 == 0) {
+        factor[r] = live ? (float)(1 << kErrorExponent) : 0.0f;
+        if (r == 0) *exponent = 0;
+    }
+    for (int c = c0; c < ld; c += 8 * tr) {
         u32x4 o = {0, 0, 0, 0};
         if (live) {
+            if (VEC) {
+                if (c < cols) {
+                    if (CODES) {
+                        const u32x2 w = *reinterpret_cast<const u32x2 *>((const uint8_t *)src + r * ld_src + c);
+                        o = __builtin_bit_cast(u32x4, halves_of((int)w.x, (int)w.y));
+                    } else {
+                        o = *reinterpret_cast<const u32x4 *>((const uint16_t *)src + r * ld_src + c);
+                    }
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                uint32_t h = 0;
-                if (c + e < cols)
-                    h = CODES ? (uint32_t)((const uint8_t *)src)[r * ld_src + c + e] << 8 : ((const uint16_t *)src)[r * ld_src + c + e];
-                o[e >> 1] |= h << (16 * (e & 1));
+                for (int e = 0; e < 8; ++e) {
+                    uint32_t h = 0;
+                    if (c + e < cols)
+                        h = CODES ? (uint32_t)((const uint8_t *)src)[r * ld_src + c + e] << 8 : ((const uint16_t *)src)[r * ld_src + c + e];
+                    o[e >> 1] |= h << (16 * (e & 1));
+                }
             }
         }
         *reinterpret_cast<u32x4 *>(dst + r * ld + c) = o;
@@ -202,6 +322,7 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t *__rest
     int e = 0;
     if (dloss != nullptr) {
         float m = 0.0f;
+#pragma unroll 4
         for (int r = threadIdx.x; r < M; r += 1024) {
             const float a = live(r) ? __builtin_fabsf(dloss[r]) : 0.0f;
             if (a < __builtin_inff()) m = __builtin_fmaxf(m, a);
@@ -217,6 +338,7 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t *__rest
         e = m > 0.0f ? ilogbf(m) + 1 : 0;
         e = e < -120 ? -120 : e > 120 ? 120 : e;
     }
+#pragma unroll 4
     for (int r = threadIdx.x; r < M; r += 1024)
         factor[r] = live(r) ? ldexpf(dloss != nullptr ? dloss[r] : 1.0f, kErrorExponent - e) : 0.0f;
     if (threadIdx.x == 0) *exponent = e;
@@ -282,13 +404,7 @@ __global__ __launch_bounds__(256) void xent_finish_kernel(const XentFinish p, in
             } else if (p.stats != nullptr) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (e < n) {
-                        if (y[e] != y[e]) st.nan_seen = 1u;
-                        st.amax = __builtin_fmaxf(st.amax, __builtin_fabsf(y[e]));
-                        st.zero_inputs += y[e] == 0.0f ? 1u : 0u;
-                        st.nonfinite += (h[e] & 0x7C00u) == 0x7C00u ? 1u : 0u;
-                        st.zero_codes += (h[e] & 0x7FFFu) == 0u ? 1u : 0u;
-                    }
+                    if (e < n) xent_count_half(st, y[e]);
             }
         }
     }
@@ -302,25 +418,6 @@ namespace {
 
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
-// Which tiles a product takes, and into how many slices its contraction is cut so that there is a workgroup for
-// every CU.
-struct Plan {
-    int tile;    // 256, 128 or 64
-    int splits;
-};
-Plan plan_tiles(int64_t rows, int64_t cols, int64_t kc, bool may_split) {
-    auto tiles = [&](int64_t t) { return ((rows + t - 1) / t) * ((cols + t - 1) / t); };
-    Plan p{64, 1};
-    if (tiles(256) >= 192) p.tile = 256;
-    else if (tiles(128) >= 192) p.tile = 128;
-    if (may_split && p.tile == 64) {
-        const int64_t steps = (kc + 63) / 64, want = 512 / tiles(64);
-        int64_t s = steps / 4 < want ? steps / 4 : want;
-        p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
-    }
-    return p;
-}
-
 struct Shape {
     int64_t M, N, K, Kp;
     bool copy_x, copy_w;
@@ -332,7 +429,7 @@ constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 bool aligned_ld(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0; }
 
 Shape make_shape(int64_t M, int64_t N, int64_t K, bool copy_x, bool copy_w, bool backward) {
-    Shape s{M, N, K, up(K, 64), copy_x, copy_w, N};
+    Shape s{M, N, K, half_pitch(K), copy_x, copy_w, N};
     // bytes per class: of e and of the FP32 sums of dw, of a copy of w
     const int64_t row_e = backward ? (2 * M > 4 * s.Kp ? 2 * M : 4 * s.Kp) : 0, row_w = copy_w ? 2 * s.Kp : 0, row = row_e > row_w ? row_e : row_w;
     if (row) {
@@ -349,21 +446,45 @@ struct Layout {
     size_t x, w, part, z_target;             // forward: copies of x and of a piece of w, the sums, the targets' logits
     size_t factor, exponent, e, dx, dw, total;  // backward: (copies as above,) the tokens' factors, e, FP32 sums
 };
+// The logits' tiles: their epilogues take longer than others, and two workgroups per CU hide them behind each other's products.  Measured,
+// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 215 / 174, 1021 x 32003 x 1000 90 / 78, 8192 x 131072 x 2048 4060 / 4540.
+HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
+    HalfPlan best = half_plan(1, M, cols, K, false, 1);
+    if (best.tile == 64) return best;
+    double least = 1e300;
+    for (const int tile : {256, 128}) {
+        const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 12.0 : 4.5;
+        const double rounds = std::ceil((double)(((M + tile - 1) / tile) * ((cols + tile - 1) / tile)) / slots);
+        const double t = rounds * ((double)((K + 63) / 64) * (tile == 256 ? 1.73 : 0.93) + epilogue);
+        if (t < least) {
+            least = t;
+            best.tile = tile;
+        }
+    }
+    return best;
+}
 int parts_of(const Shape &s) {  // sums per token
     int n = 0;
     for (int64_t c = 0; c < s.N; c += s.piece) {
         const int64_t cols = s.N - c < s.piece ? s.N - c : s.piece;
-        const int w = plan_tiles(s.M, cols, s.K, false).tile / 2;
+        const int w = logits_plan(s.M, cols, s.K).tile;
         n += (int)((cols + w - 1) / w);
     }
     return n;
 }
+// dx and dw.  A tile that holds the complete sum stores the gradient itself where a row is whole groups of eight; otherwise FP32 sums
+// (of every slice; of all pieces, for dx) pass through the workspace.
 struct BwdPlans {
-    Plan dx, dw;
+    HalfPlan dx, dw;
+    bool dx_direct, dw_direct;
 };
 BwdPlans bwd_plans(const Shape &s) {
-    const int64_t n = s.piece < s.N ? s.piece : s.N;
-    return {plan_tiles(s.M, s.K, n, true), plan_tiles(n, s.K, s.M, true)};
+    BwdPlans p;
+    p.dx = half_plan(1, s.M, s.K, s.piece, false, 64);
+    p.dw = half_plan(1, s.piece, s.K, s.M, false, 64);
+    p.dx_direct = s.K % 8 == 0 && p.dx.splits == 1 && s.piece >= s.N;
+    p.dw_direct = s.K % 8 == 0 && p.dw.splits == 1;
+    return p;
 }
 Layout make_layout(const Shape &s, bool backward, bool dx, bool dw) {
     Layout l{};
@@ -381,10 +502,10 @@ Layout make_layout(const Shape &s, bool backward, bool dx, bool dw) {
     } else {
         l.factor = take(4 * s.M);
         l.exponent = take(4);
-        l.e = take(2 * s.M * up(s.piece, 64));
+        l.e = take(2 * s.M * half_pitch(s.piece));
         const BwdPlans p = bwd_plans(s);
-        if (dx) l.dx = take(4 * p.dx.splits * s.M * s.Kp);
-        if (dw) l.dw = take(4 * p.dw.splits * s.piece * s.Kp);
+        if (dx && !p.dx_direct) l.dx = take(4 * p.dx.splits * s.M * s.Kp);
+        if (dw && !p.dw_direct) l.dw = take(4 * p.dw.splits * s.piece * s.Kp);
     }
     l.total = at;
     return l;
@@ -411,11 +532,14 @@ bool product(int tile, const void *a, int64_t lda, const void *b, int64_t ldb, i
 }
 
 bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t ld, int64_t rows, int64_t cols,
-               const int64_t *targets, int64_t N, hipStream_t stream) {
-    if (codes)
-        hipLaunchKernelGGL((xent_copy_kernel<true>), dim3((unsigned)rows), dim3(256), 0, stream, src, ld_src, dst, ld, (int)cols, targets, (int)N);
-    else
-        hipLaunchKernelGGL((xent_copy_kernel<false>), dim3((unsigned)rows), dim3(256), 0, stream, src, ld_src, dst, ld, (int)cols, targets, (int)N);
+               const int64_t *targets, int64_t N, float *factor, int *exponent, hipStream_t stream) {
+    int tr = 1;
+    while (tr < 256 && 8 * tr < ld) tr *= 2;
+    const bool vec = cols % 8 == 0 && ld_src % 8 == 0;
+    const auto kernel = codes ? (vec ? xent_copy_kernel<true, true> : xent_copy_kernel<true, false>)
+                              : (vec ? xent_copy_kernel<false, true> : xent_copy_kernel<false, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / tr - 1) / (256 / tr))), dim3(256), 0, stream, src, ld_src, dst, ld, (int)rows, (int)cols,
+                       targets, (int)N, tr, factor, exponent);
     return hipGetLastError() == hipSuccess;
 }
 
@@ -452,7 +576,7 @@ extern "C" mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K,
     int64_t ld_x = ldx;
     if (s.copy_x) {
         xs = (uint16_t *)(ws + l.x);
-        if (!copy_half(x, x_is_e5m2 != 0, ldx, (uint16_t *)(ws + l.x), s.Kp, M, K, nullptr, N, st)) return MP8_ERR_HIP;
+        if (!copy_half(x, x_is_e5m2 != 0, ldx, (uint16_t *)(ws + l.x), s.Kp, M, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
         ld_x = s.Kp;
     }
     int parts = 0;
@@ -461,16 +585,17 @@ extern "C" mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K,
         const uint16_t *wp = w + c * ldw;
         int64_t ld_w = ldw;
         if (s.copy_w) {
-            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, st)) return MP8_ERR_HIP;
+            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
             wp = (uint16_t *)(ws + l.w);
             ld_w = s.Kp;
         }
-        const int tile = plan_tiles(M, cols, K, false).tile;
+        const int tile = logits_plan(M, cols, K).tile;
         const XentStats epi{targets, (f32x2 *)(ws + l.part), (float *)(ws + l.z_target), (int)M, (int)cols, (int)c, parts};
         if (!product<false, false>(tile, xs, ld_x, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
-        parts += (int)((cols + tile / 2 - 1) / (tile / 2));
+        parts += (int)((cols + tile - 1) / tile);
     }
-    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((M + 31) / 32)), dim3(256), 0, st, (const f32x2 *)(ws + l.part), (const float *)(ws + l.z_target),
+    const int per = M >= 512 ? 8 : 1;
+    hipLaunchKernelGGL((per == 8 ? xent_join_kernel<8> : xent_join_kernel<1>), dim3((unsigned)((M + per - 1) / per)), dim3(256), 0, st, (const f32x2 *)(ws + l.part), (const float *)(ws + l.z_target),
                        targets, loss, lse, (int)M, (int)N, parts);
     return hipGetLastError() == hipSuccess ? MP8_OK : MP8_ERR_HIP;
 }
@@ -500,10 +625,12 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     uint16_t *xs = (uint16_t *)(ws + l.x), *e = (uint16_t *)(ws + l.e);
     float *factor = (float *)(ws + l.factor), *dxs = (float *)(ws + l.dx), *dws = (float *)(ws + l.dw);
     int *exponent = (int *)(ws + l.exponent);
-    if (!copy_half(x, x_is_e5m2 != 0, ldx, xs, s.Kp, M, K, targets, N, st)) return MP8_ERR_HIP;
-    hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, dloss, factor, exponent, (int)M, (int)N);
-    if (hipGetLastError() != hipSuccess) return MP8_ERR_HIP;
-    const int64_t K8 = up(K, 8), lde = up(s.piece, 64);
+    if (!copy_half(x, x_is_e5m2 != 0, ldx, xs, s.Kp, M, K, targets, N, dloss ? nullptr : factor, exponent, st)) return MP8_ERR_HIP;
+    if (dloss) {
+        hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, dloss, factor, exponent, (int)M, (int)N);
+        if (hipGetLastError() != hipSuccess) return MP8_ERR_HIP;
+    }
+    const int64_t K8 = up(K, 8), lde = half_pitch(s.piece);
     const BwdPlans plans = bwd_plans(s);
     auto finish = [&](const float *sum, int64_t slab, int slabs, int64_t rows, int64_t row0, uint16_t *out16, uint8_t *out8, uint64_t offset,
                       mp8_stats *stats) {
@@ -516,27 +643,49 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
         hipLaunchKernelGGL(xent_finish_kernel, dim3((unsigned)blocks), dim3(256), 0, st, f, tr);
         return hipGetLastError() == hipSuccess;
     };
+    // (a, b) -> rows [row0, row0 + rows) of a gradient, complete
+    auto direct = [&](auto atn, int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
+                      uint8_t *out8, uint64_t offset, mp8_stats *stats) {
+        constexpr bool ATN = decltype(atn)::value;
+        const int64_t rows_a = ATN ? up(rows, 8) : rows;
+        auto epi = [&](auto full) {
+            return XentOut<decltype(full)::value>{exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0,
+                                                  seed, offset, stats};
+        };
+        if (out8 == nullptr && stats == nullptr) return product<true, ATN>(tile, a, lda, b, ldb, rows_a, K8, kc, 1, epi(std::false_type{}), st);
+        const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows_a, K8, kc, tile == 64 ? 64 : 128, tile == 64 ? 64 : 128, 1, false);
+        return tile == 64 ? half_gemm_launch<Half64, ATN, true>(p, 1, epi(std::true_type{}), st)
+                          : half_gemm_launch<Half128, ATN, true>(p, 1, epi(std::true_type{}), st);
+    };
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
         const uint16_t *wp = w + c * ldw;
         int64_t ld_w = ldw;
         if (s.copy_w) {
-            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, st)) return MP8_ERR_HIP;
+            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
             wp = (uint16_t *)(ws + l.w);
             ld_w = s.Kp;
         }
         const XentError epi{targets, loss, lse, factor, e, lde, (int)M, (int)cols, (int)c};
-        if (!product<false, false>(plan_tiles(M, cols, K, false).tile, xs, s.Kp, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        if (!product<false, false>(logits_plan(M, cols, K).tile, xs, s.Kp, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
         if (dx) {
-            const HalfEpiSum sum{dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
-            if (!product<true, false>(plans.dx.tile, e, lde, wp, ld_w, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
+            if (plans.dx_direct) {
+                if (!direct(std::false_type{}, plans.dx.tile, e, lde, wp, ld_w, M, cols, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
+            } else {
+                const HalfEpiSum sum{dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
+                if (!product<true, false>(plans.dx.tile, e, lde, wp, ld_w, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
+            }
         }
         if (dw) {
-            const HalfEpiSum sum{dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
-            if (!product<true, true>(plans.dw.tile, e, lde, xs, s.Kp, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
-            if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
+            if (plans.dw_direct) {
+                if (!direct(std::true_type{}, plans.dw.tile, e, lde, xs, s.Kp, cols, M, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
+            } else {
+                const HalfEpiSum sum{dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
+                if (!product<true, true>(plans.dw.tile, e, lde, xs, s.Kp, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
+                if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
+            }
         }
     }
-    if (dx && !finish(dxs, M * s.Kp, plans.dx.splits, M, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
+    if (dx && !plans.dx_direct && !finish(dxs, M * s.Kp, plans.dx.splits, M, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
     return MP8_OK;
 }
