@@ -75,6 +75,7 @@ struct HalfTiling {
     static constexpr bool WHOLE = WHOLE_;
 };
 using Half256 = HalfTiling<256, 256, 2, 1, false>;
+using Half192 = HalfTiling<192, 192, 2, 1, false>;
 using Half128 = HalfTiling<128, 128, 2, 2, true>;
 using Half64 = HalfTiling<64, 64, 4, 2, true>;
 using f32x2 = float __attribute__((ext_vector_type(2)));
@@ -85,6 +86,7 @@ struct HalfPlace {
     int batch, split, tm, tn;
     int row0, col0;  // of the wave's part
     int wave, lane;
+    uint8_t *lds;    // the operand ring, which other waves may still be reading
     __device__ __forceinline__ int row(int i) const { return row0 + 32 * i + (lane & 31); }
     __device__ __forceinline__ int col(int j) const { return col0 + 32 * j + 4 * (lane >> 5); }
 };
@@ -281,7 +283,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
             }
         }
     }
-    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane};
+    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane, lds};
     epi(at, acc);
 }
 
@@ -296,8 +298,53 @@ __device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
     return u32x4{s0[0], s1[0], s0[1], s1[1]};
 }
 
+// f(r, c, v) for every eight neighbouring columns c .. c+7 of rows r of the wave's part: bands of 32 rows pass through LDS (a
+// region of the ring per wave), so that f's code is there once per band, and the lanes that share a row lie side by side: stores
+// and loads of whole 128-byte lines.  before(i, band): called when
+// the i-th one lies in LDS, 32 rows of PITCH floats.
+template <class T>
+constexpr int kHalfBandPitch = T::WTN + 4;
+template <class T, class F, class Between>
+__device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f, const Between &before) {
+    constexpr int PITCH = kHalfBandPitch<T>, PER = T::WTN / 8, ROWS = 64 / PER;  // lanes of a row, rows of a pass (192: 5 rows, 60 lanes)
+    static_assert(4 * 32 * PITCH * 4 <= T::NSTAGE * (T::BM + T::BN) * 128, "the bands fit the ring");
+    float *band = reinterpret_cast<float *>(at.lds) + at.wave * 32 * PITCH;
+    const int lr = at.lane / PER, lc = 8 * (at.lane % PER);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < T::MT; ++i) {
+#pragma unroll
+        for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                *reinterpret_cast<f32x4 *>(band + (at.lane & 31) * PITCH + 32 * j + 8 * g + 4 * (at.lane >> 5)) = v;
+            }
+        before(i, band);
+#pragma unroll 1
+        for (int k = lr; k < 32; k += ROWS) {
+            if (64 % PER != 0 && lr >= ROWS) break;
+            const f32x4 lo = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc), hi = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc + 4);
+            const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            f(at.row0 + 32 * i + k, at.col0 + lc, v);
+        }
+    }
+}
+template <class T, class F>
+__device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f) {
+    half_bands(at, acc, f, [](int, float *) {});
+}
+
+// Eight halves from eight FP32 values, to nearest.
+__device__ __forceinline__ u32x4 half_round8(const float v[8]) {
+    u32x4 w;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) w[q] = f16_from_f32<false>(v[2 * q], 0u) | f16_from_f32<false>(v[2 * q + 1], 0u) << 16;
+    return w;
+}
+
 // The FP32 tile itself, scaled by nothing, stored or added to what is there: slab `split` of [rows, ld] floats (ld a multiple of
-// 32 and at least the columns, so that whole rows of 32 may be stored).
+// eight and at least the columns, so that whole groups of eight may be stored).
 struct HalfEpiSum {
     float *out;
     int64_t ld, slab, batch;  // in floats
@@ -305,33 +352,17 @@ struct HalfEpiSum {
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
         float *base = out + at.batch * batch + at.split * slab;
-#pragma unroll
-        for (int i = 0; i < T::MT; ++i) {
-            const int r = at.row(i);
-#pragma unroll
-            for (int j = 0; j < T::NT; ++j) {
-                if (at.col0 + 32 * j >= cols) break;
-#pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    f32x4 lo, hi;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const auto s = __builtin_amdgcn_permlane32_swap(f2u(acc[i][j][4 * g + e]), f2u(acc[i][j][4 * g + 4 + e]), false, false);
-                        lo[e] = u2f(s[0]);
-                        hi[e] = u2f(s[1]);
-                    }
-                    if (r < rows) {
-                        f32x4 *to = reinterpret_cast<f32x4 *>(base + r * ld + at.col0 + 32 * j + 8 * g + 8 * (at.lane >> 5));
-                        if (add) {
-                            lo += to[0];
-                            hi += to[1];
-                        }
-                        to[0] = lo;
-                        to[1] = hi;
-                    }
-                }
+        half_bands(at, acc, [&](int r, int c, const float (&v)[8]) {
+            if (r >= rows || c >= cols) return;
+            f32x4 *to = reinterpret_cast<f32x4 *>(base + r * ld + c);
+            f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+            if (add) {
+                lo += to[0];
+                hi += to[1];
             }
-        }
+            to[0] = lo;
+            to[1] = hi;
+        });
     }
 };
 
@@ -347,21 +378,22 @@ struct HalfPlan {
 };
 
 // Estimated time, us, of `tiles` tiles over `stages` stages.  Measured (4096 x 4096 x 4096 and parts of it), us per stage: 64x64 tiles, up to 256
-// of them 0.25, up to 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93; 256x256, 128 1.36, 256 1.73; more tiles take rounds.  On top
-// come start and end of a workgroup.
+// of them 0.25, 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93; 192x192, 64 0.81, 256 1.06; 256x256, 128 1.36, 256 1.73; more tiles
+// take rounds.  On top come start and end of a workgroup.
 static inline double half_cost(int tile, int64_t tiles, double stages) {
-    const int64_t slots = tile == 256 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
-    const double whole = tile == 256 ? 1.73 : tile == 128 ? 0.93 : 0.41, half = tile == 256 ? 1.36 : tile == 128 ? 0.69 : 0.25;
-    const double base = tile == 256 ? 10.0 : tile == 128 ? 5.0 : 3.5;
-    const double rounds = (double)(full + (rest != 0));
-    return base * (rounds < 1 ? 1 : 0.5 + 0.5 * rounds) + stages * ((double)full * whole + (rest == 0 ? 0.0 : rest <= slots / 2 ? half : whole));
+    const int64_t slots = tile > 128 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
+    const double whole = tile == 256 ? 1.73 : tile == 192 ? 1.06 : tile == 128 ? 0.93 : 0.41, half = tile == 256 ? 1.36 : tile == 192 ? 0.85 : tile == 128 ? 0.69 : 0.25;
+    const double base = tile == 256 ? 10.0 : tile == 192 ? 8.0 : tile == 128 ? 5.0 : 3.5;
+    const double rounds = (double)(full + (rest != 0)), over = (double)(rest - slots / 2) / (double)(slots / 2);
+    const double part = rest == 0 ? 0.0 : over <= 0.0 ? half : half + over * (whole - half);
+    return base * (rounds < 1 ? 1 : 0.5 + 0.5 * rounds) + stages * ((double)full * whole + part);
 }
 
 // most_splits > 1: the slices' FP32 sums are written and added up by a pass of its own.
 static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int64_t kc, bool symmetric, int most_splits) {
     HalfPlan best{64, 1};
     double least = 1e300;
-    for (const int tile : {256, 128, 64}) {
+    for (const int tile : {256, 192, 128, 64}) {
         const int64_t tm = (rows + tile - 1) / tile, tn = (cols + tile - 1) / tile;
         const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn), steps = (kc + 63) / 64;
         if (tiles > (int64_t)1 << 23) continue;

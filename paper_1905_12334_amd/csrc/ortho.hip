@@ -7,7 +7,8 @@
 // A step maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors alone: with (a, b, c) = (3.4445,
 // -4.7750, 2.0315), whose slope at zero is steep, five steps bring all but the smallest to 0.7 .. 1.2.
 //
-// X lies with its shorter side (m) as rows, whatever the weights' layout, so that A is m x m.  Operands of the products are
+// X lies as the weights do, [rows, ld].  A is formed over the shorter side: X X^T and (bA + cA^2) X where rows <= cols, X^T X and
+// X (bA + cA^2) otherwise; the second product of the last step updates the weights itself.  Operands of the products are
 // halves, sums FP32.  A power of two keeps each of them in the format's range: singular values stay below 1.21, so that entries of A
 // are below 1.46 and those of bA + cA^2 below 2.81 in magnitude; A and the polynomial are stored times 2^14, X times S = 2^round(log2
 // sqrt n), which makes the entries of an orthogonal X about 1.  What half operands cost: entries of X are off by 1.3e-3 of
@@ -23,89 +24,138 @@ constexpr float kOrthoA = 3.4445f, kOrthoB = -4.7750f, kOrthoC = 2.0315f;
 constexpr float kUp = 16384.0f, kDown = 1.0f / 16384.0f;  // the scale of A and of the polynomial
 
 // A symmetric output of halves, made from its upper tiles: v = linear * in[r, c] + scale * acc at (r, c) and, off the diagonal's
-// tiles, at (c, r).
+// tiles, at (c, r), turned round by the lanes that read the band.  Columns m .. m8 - 1 are zero.
 struct OrthoSymmetric {
     const uint16_t *in;  // nullable
     uint16_t *out;
     int64_t ld, batch;   // in halves
-    int m;               // rows and columns that are stored (a multiple of 8)
+    int m;
     float linear, scale;
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
         const uint16_t *x = in != nullptr ? in + at.batch * batch : nullptr;
         uint16_t *o = out + at.batch * batch;
         const bool mirror = at.tm != at.tn;
+        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+            if (r >= m || c >= m) return;
+            u32x4 xw = {0, 0, 0, 0};
+            if (x != nullptr) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
+            *reinterpret_cast<u32x4 *>(o + r * ld + c) = value(xw, sum, m - c);
+        }, [&](int i, const float *band) {
+            if (!mirror) return;
+            // four lanes per row of the turned band: its rows are the band's columns, its columns rows of the tile, all of which exist
+            // (a tile below the diagonal's ends at a tile border)
+            const int k = 8 * (at.lane & 3), r = at.row0 + 32 * i + k;
+#pragma unroll 1
+            for (int n = at.lane >> 2; n < T::WTN; n += 16) {
+                const int c = at.col0 + n;
+                if (c >= m) break;
+                float sum[8];
 #pragma unroll
-        for (int i = 0; i < T::MT; ++i) {
-            const int r = at.row(i);
-#pragma unroll
-            for (int j = 0; j < T::NT; ++j) {
-                if (at.col0 + 32 * j >= m) break;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int c = at.col(j) + 8 * g;
-                    if (r >= m || c >= m) continue;
-                    float v[4];
-                    uint32_t h[4];
-                    u32x2 xw = {0, 0};
-                    if (x != nullptr) xw = *reinterpret_cast<const u32x2 *>(x + r * ld + c);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        v[e] = scale * acc[i][j][4 * g + e];
-                        if (x != nullptr) v[e] = __builtin_fmaf(linear, half_bits_to_f32((e < 2 ? xw.x : xw.y) >> (16 * (e & 1))), v[e]);
-                        h[e] = f16_from_f32<false>(v[e], 0u);
-                    }
-                    const u32x2 w = {h[0] | (h[1] << 16), h[2] | (h[3] << 16)};
-                    *reinterpret_cast<u32x2 *>(o + r * ld + c) = w;
-                    if (mirror) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[(c + e) * ld + r] = (uint16_t)h[e];
-                    }
-                }
+                for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
+                u32x4 xw = {0, 0, 0, 0};
+                if (x != nullptr) xw = *reinterpret_cast<const u32x4 *>(x + c * ld + r);
+                *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw, sum, 8);
             }
+        });
+    }
+    __device__ __forceinline__ u32x4 value(const u32x4 &xw, const float (&sum)[8], int left) const {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[e] = __builtin_fmaf(linear, half_bits_to_f32(xw[e >> 1] >> (16 * (e & 1))), scale * sum[e]);
+            if (e >= left) v[e] = 0.0f;
         }
+        return half_round8(v);
     }
 };
 
-// The next iterate, a X + scale * acc, as halves; or, after the last step, as FP32 without X's scale.
+// The next iterate, a X + scale * acc, as halves.  Columns up to the next multiple of eight are stored (they are zero).
 struct OrthoNext {
     const uint16_t *x;
-    uint16_t *out;     // null after the last step
-    float *last;
-    int64_t ld, batch; // in elements
-    int m, n;          // stored rows and columns (n a multiple of 8)
-    float inv_s;
+    uint16_t *out;
+    int64_t ld, batch; // in halves
+    int rows, cols;
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+            if (r >= rows || c >= cols) return;
+            const int64_t i0 = at.batch * batch + r * ld + c;
+            const u32x4 xw = *reinterpret_cast<const u32x4 *>(x + i0);
+            float v[8];
 #pragma unroll
-        for (int i = 0; i < T::MT; ++i) {
-            const int r = at.row(i);
+            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(kOrthoA, half_bits_to_f32(xw[e >> 1] >> (16 * (e & 1))), kDown * sum[e]);
+            *reinterpret_cast<u32x4 *>(out + i0) = half_round8(v);
+        });
+    }
+};
+
+// The last iterate goes straight into the weights: w' = w - lr (X + wd w), rounded to half, and its 8-bit copy.
+struct OrthoUpdate {
+    const uint16_t *x;
+    int64_t ld, batch;
+    int rows, cols;
+    float inv_s, neg_lr, wd;
+    uint16_t *w16;
+    uint8_t *w8;
+    int sr;
+    uint64_t seed, offset;
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+        const Philox rng(seed, offset);
+        const bool whole = (cols & 7) == 0;
+        const int64_t first = (int64_t)at.batch * rows * cols;
+        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+            if (r >= rows || c >= cols) return;
+            const u32x4 xw = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + r * ld + c);
+            const int64_t i0 = first + (int64_t)r * cols + c;
+            const int n = cols - c < 8 ? cols - c : 8;
+            u32x4 ww = {0, 0, 0, 0};
+            if (whole) {
+                ww = *reinterpret_cast<const u32x4 *>(w16 + i0);
+            } else {
 #pragma unroll
-            for (int j = 0; j < T::NT; ++j) {
-                if (at.col0 + 32 * j >= n) break;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int c = at.col(j) + 8 * g;
-                    if (r >= m || c >= n) continue;
-                    const int64_t i0 = at.batch * batch + r * ld + c;
-                    const u32x2 xw = *reinterpret_cast<const u32x2 *>(x + i0);
-                    float v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        v[e] = __builtin_fmaf(kOrthoA, half_bits_to_f32((e < 2 ? xw.x : xw.y) >> (16 * (e & 1))), kDown * acc[i][j][4 * g + e]);
-                    if (out != nullptr) {
-                        uint32_t h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) h[e] = f16_from_f32<false>(v[e], 0u);
-                        const u32x2 w = {h[0] | (h[1] << 16), h[2] | (h[3] << 16)};
-                        *reinterpret_cast<u32x2 *>(out + i0) = w;
-                    } else {
-                        const f32x4 o = {v[0] * inv_s, v[1] * inv_s, v[2] * inv_s, v[3] * inv_s};
-                        *reinterpret_cast<f32x4 *>(last + i0) = o;
-                    }
+                for (int e = 0; e < 8; ++e)
+                    if (e < n) ww[e >> 1] |= (uint32_t)w16[i0 + e] << (16 * (e & 1));
+            }
+            uint32_t rw[4] = {0, 0, 0, 0};
+            if (sr) {
+                if (whole) {
+                    const uint4 b = rng.block((uint64_t)i0 >> 3);
+                    rw[0] = b.x; rw[1] = b.y; rw[2] = b.z; rw[3] = b.w;
+                } else {
+                    const Words4 a = rng.words_at((uint64_t)i0), b = rng.words_at((uint64_t)i0 + 4);
+                    rw[0] = a.r01; rw[1] = a.r23; rw[2] = b.r01; rw[3] = b.r23;
                 }
             }
-        }
+            u32x4 o;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t hw[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float d = __builtin_fmaf(kOrthoA, half_bits_to_f32(xw[q] >> (16 * e)), kDown * sum[2 * q + e]) * inv_s;
+                    const float f = half_bits_to_f32(ww[q] >> (16 * e));
+                    float wn = __builtin_fmaf(neg_lr, __builtin_fmaf(wd, f, d), f);
+                    asm volatile("" : "+v"(wn));  // (two roundings: see update_four)
+                    hw[e] = sr ? f16_from_f32<true>(wn, e ? rw[q] & 0xFFFF0000u : rw[q] << 16) : f16_from_f32<false>(wn, 0u);
+                }
+                o[q] = hw[0] | (hw[1] << 16);
+            }
+            const uint32_t lo[2] = {o.x, o.y}, hi[2] = {o.z, o.w};
+            const u32x2 codes = {w8 != nullptr ? e5m2_of_halves(lo) : 0u, w8 != nullptr ? e5m2_of_halves(hi) : 0u};
+            if (whole) {
+                *reinterpret_cast<u32x4 *>(w16 + i0) = o;
+                if (w8 != nullptr) *reinterpret_cast<u32x2 *>(w8 + i0) = codes;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < n) {
+                        w16[i0 + e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
+                        if (w8 != nullptr) w8[i0 + e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
+                    }
+            }
+        });
     }
 };
 
@@ -175,13 +225,11 @@ __global__ __launch_bounds__(256) void ortho_momentum_kernel(const OrthoMomentum
     }
 }
 
-// X0 times S as halves, [m8, ld] per matrix, from the new momentum and the gradient: a workgroup per 64x64 tile, transposed through
-// LDS where the weights are taller than wide.  Zeros beyond m and n.
+// X0 times S as halves, [rows, ld] per matrix, from the new momentum and the gradient: eight columns per thread, zeros behind the last.
 struct OrthoStart {
     const float *v;
     const uint8_t *g8;
-    int rows, cols;   // of the weights
-    int transposed;
+    int rows, cols;
     float inv_scale, mu;
     int nesterov, blocks;
     const double *squares;
@@ -189,113 +237,53 @@ struct OrthoStart {
     double s;
     uint16_t *x;
     int64_t ld, batch;
-    int m8;
+    FastDiv div_groups;  // by the groups of eight in a row, cols / 8 rounded up
 };
 __global__ __launch_bounds__(256) void ortho_start_kernel(const OrthoStart p) {
-    __shared__ uint16_t sh[64][66];
+    const uint32_t groups = (uint32_t)p.rows * p.div_groups.d, stride = gridDim.x * 256;
+    const int64_t base = (int64_t)blockIdx.y * p.rows * p.cols;
+    const bool whole = (p.cols & 7) == 0;
     if (p.skip != nullptr && *p.skip != 0u) return;
-    double sum = 0.0;
-    for (int b = threadIdx.x & 63; b < p.blocks; b += 64) sum += p.squares[(int64_t)blockIdx.z * p.blocks + b];
+    double sum = 0.0;  // (by all lanes of the wave, also those without a group)
+    for (int b = threadIdx.x & 63; b < p.blocks; b += 64) sum += p.squares[(int64_t)blockIdx.y * p.blocks + b];
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
     const double inv = sum == 0.0 ? 0.0 : p.s / sqrt(sum);
-    // tile of the weights' matrix
-    const int r0 = 64 * (p.transposed ? blockIdx.x : blockIdx.y), c0 = 64 * (p.transposed ? blockIdx.y : blockIdx.x);
-    const int64_t base = (int64_t)blockIdx.z * p.rows * p.cols;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int r = r0 + y + 4 * k, c = c0 + x;
-        uint32_t h = 0;
-        if (r < p.rows && c < p.cols) {
-            const int64_t i = base + (int64_t)r * p.cols + c;
-            const float g = e5m2_to_f32(p.g8[i]) * p.inv_scale;
-            h = f16_from_f32<false>((float)((double)ortho_direction(p.v[i], g, p.mu, p.nesterov) * inv), 0u);
-        }
-        sh[y + 4 * k][x] = (uint16_t)h;
-    }
-    __syncthreads();
-    uint16_t *out = p.x + blockIdx.z * p.batch;
-#pragma unroll 4
-    for (int k = 0; k < 16; ++k) {
-        const int r = 64 * blockIdx.y + y + 4 * k, c = 64 * blockIdx.x + x;  // of X
-        if (r < p.m8) out[r * p.ld + c] = p.transposed ? sh[x][y + 4 * k] : sh[y + 4 * k][x];
-    }
-}
-
-// w' = w - lr (X + wd w), rounded to half, and its 8-bit copy.  A workgroup per 64x64 tile of the weights.
-struct OrthoApply {
-    const float *o;
-    int64_t ld, batch;
-    int rows, cols, transposed;
-    uint16_t *w16;
-    uint8_t *w8;
-    float neg_lr, wd;
-    int sr;
-    uint64_t seed, offset;
-    const uint32_t *skip;
-};
-__global__ __launch_bounds__(256) void ortho_apply_kernel(const OrthoApply p) {
-    __shared__ float sh[64][65];
-    if (p.skip != nullptr && *p.skip != 0u) return;
-    const int r0 = 64 * blockIdx.y, c0 = 64 * blockIdx.x;
-    const float *o = p.o + blockIdx.z * p.batch;
-    const int64_t base = (int64_t)blockIdx.z * p.rows * p.cols;
-    const int x = threadIdx.x & 63, y = threadIdx.x >> 6;
-    if (p.transposed) {
-#pragma unroll 4
-        for (int k = 0; k < 16; ++k) {
-            const int c = c0 + y + 4 * k, r = r0 + x;  // row c of X, column r
-            sh[x][y + 4 * k] = c < p.cols && r < p.rows ? o[c * p.ld + r] : 0.0f;
-        }
-        __syncthreads();
-    }
-    const Philox rng(p.seed, p.offset);
-    // four neighbouring columns per thread
-    const int cx = 4 * (threadIdx.x & 15), ry = threadIdx.x >> 4;
-    const bool whole = (p.cols & 3) == 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const int lr = ry + 16 * k, r = r0 + lr, c = c0 + cx;
-        if (r >= p.rows || c >= p.cols) continue;
+    for (uint32_t t = blockIdx.x * 256 + threadIdx.x; t < groups; t += stride) {
+        uint32_t k;
+        const uint32_t r = fastdiv(t, p.div_groups, k);
+        const int c = 8 * (int)k;
         const int64_t i = base + (int64_t)r * p.cols + c;
-        const int n = p.cols - c < 4 ? p.cols - c : 4;
-        float d[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = p.transposed ? sh[lr][cx + e] : e < n ? o[r * p.ld + c + e] : 0.0f;
-        uint32_t w[4], h[4];
+        uint32_t code[2] = {0, 0};
+        float v[8];
         if (whole) {
-            const u32x2 in = *reinterpret_cast<const u32x2 *>(p.w16 + i);
-            w[0] = in.x & 0xFFFFu; w[1] = in.x >> 16; w[2] = in.y & 0xFFFFu; w[3] = in.y >> 16;
+            const u32x2 g = *reinterpret_cast<const u32x2 *>(p.g8 + i);
+            const f32x4 a = *reinterpret_cast<const f32x4 *>(p.v + i), b = *reinterpret_cast<const f32x4 *>(p.v + i + 4);
+            code[0] = g.x;
+            code[1] = g.y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
         } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = e < n ? p.w16[i + e] : 0u;
-        }
-        Words4 words = {0, 0};
-        if (p.sr) words = rng.words_at((uint64_t)i);
-        const uint32_t rw[4] = {words.r01 << 16, words.r01 & 0xFFFF0000u, words.r23 << 16, words.r23 & 0xFFFF0000u};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float f = half_bits_to_f32(w[e]);
-            float wn = __builtin_fmaf(p.neg_lr, __builtin_fmaf(p.wd, f, d[e]), f);
-            asm volatile("" : "+v"(wn));  // (two roundings: see update_four)
-            h[e] = p.sr ? f16_from_f32<true>(wn, rw[e]) : f16_from_f32<false>(wn, 0u);
-        }
-        if (whole) {
-            const u32x2 out = {h[0] | (h[1] << 16), h[2] | (h[3] << 16)};
-            *reinterpret_cast<u32x2 *>(p.w16 + i) = out;
-            if (p.w8 != nullptr) {
-                const uint32_t two[2] = {out.x, out.y};
-                *reinterpret_cast<uint32_t *>(p.w8 + i) = e5m2_of_halves(two);
+            for (int e = 0; e < 8; ++e) {
+                const bool in = c + e < p.cols;
+                code[e >> 2] |= (in ? (uint32_t)p.g8[i + e] : 0u) << (8 * (e & 3));
+                v[e] = in ? p.v[i + e] : 0.0f;
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) {
-                    p.w16[i + e] = (uint16_t)h[e];
-                    if (p.w8 != nullptr) p.w8[i + e] = (uint8_t)e5m2_of_half(h[e]);
-                }
         }
+        u32x4 o;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            uint32_t h[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int n = 2 * q + e;
+                const float g = e5m2_to_f32((code[n >> 2] >> (8 * (n & 3))) & 0xFFu) * p.inv_scale;
+                h[e] = f16_from_f32<false>((float)((double)ortho_direction(v[n], g, p.mu, p.nesterov) * inv), 0u);
+            }
+            o[q] = h[0] | (h[1] << 16);
+        }
+        *reinterpret_cast<u32x4 *>(p.x + blockIdx.y * p.batch + r * p.ld + c) = o;
     }
 }
 
@@ -307,17 +295,15 @@ namespace {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct OrthoLayout {
-    int64_t m, n, m8, n8, ld, lda;  // X [m8, ld], A [m8, lda]
-    int blocks;                     // workgroups of the momentum pass per matrix
-    size_t squares, x0, x1, a, b, last, total;
+    int64_t m, n, ld, lda;  // shorter and longer side; X [rows, ld], A [m, lda]
+    int blocks;             // workgroups of the momentum pass per matrix
+    size_t squares, x0, x1, a, b, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     OrthoLayout l{};
     l.m = rows < cols ? rows : cols;
     l.n = rows < cols ? cols : rows;
-    l.m8 = up(l.m, 8);
-    l.n8 = up(l.n, 8);
-    l.ld = half_pitch(l.n);
+    l.ld = half_pitch(cols);
     l.lda = half_pitch(l.m);
     const int64_t want = (rows * cols + 4095) / 4096, most = batch >= 256 ? 4 : 1024 / batch;
     l.blocks = (int)(want < 1 ? 1 : want > most ? most : want);
@@ -328,11 +314,10 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
         return here;
     };
     l.squares = take(8 * batch * l.blocks);
-    l.x0 = take(2 * batch * l.m8 * l.ld);
-    l.x1 = take(2 * batch * l.m8 * l.ld);
-    l.a = take(2 * batch * l.m8 * l.lda);
-    l.b = take(2 * batch * l.m8 * l.lda);
-    l.last = take(4 * batch * l.m8 * l.ld);
+    l.x0 = take(2 * batch * rows * l.ld);
+    l.x1 = take(2 * batch * rows * l.ld);
+    l.a = take(2 * batch * l.m * l.lda);
+    l.b = take(2 * batch * l.m * l.lda);
     l.total = at;
     return l;
 }
@@ -347,15 +332,20 @@ mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
     return MP8_OK;
 }
 
-template <bool BTN, class Epi>
-bool ortho_product(int64_t batch, const uint16_t *a, int64_t lda, int64_t a_batch, const uint16_t *b, int64_t ldb, int64_t b_batch, int64_t rows,
-                   int64_t cols, int64_t kc, bool symmetric, const uint32_t *skip, const Epi &epi, hipStream_t stream) {
+struct OrthoOperand {
+    const uint16_t *p;
+    int64_t ld, batch;
+};
+template <bool ATN, bool BTN, class Epi>
+bool ortho_product(int64_t batch, const OrthoOperand &a, const OrthoOperand &b, int64_t rows, int64_t cols, int64_t kc, bool symmetric,
+                   const uint32_t *skip, const Epi &epi, hipStream_t stream) {
     const int tile = half_plan(batch, rows, cols, kc, symmetric, 1).tile;
-    HalfGemm p = half_gemm_args(a, lda, a_batch, b, ldb, b_batch, rows, cols, kc, tile, tile, 1, symmetric);
+    HalfGemm p = half_gemm_args(a.p, a.ld, a.batch, b.p, b.ld, b.batch, rows, cols, kc, tile, tile, 1, symmetric);
     p.skip = skip;
-    if (tile == 256) return half_gemm_launch<Half256, false, BTN>(p, batch, epi, stream);
-    if (tile == 128) return half_gemm_launch<Half128, false, BTN>(p, batch, epi, stream);
-    return half_gemm_launch<Half64, false, BTN>(p, batch, epi, stream);
+    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, batch, epi, stream);
+    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, batch, epi, stream);
+    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, batch, epi, stream);
+    return half_gemm_launch<Half64, ATN, BTN>(p, batch, epi, stream);
 }
 
 }  // namespace
@@ -388,29 +378,35 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     hipStream_t st = (hipStream_t)stream;
     double *squares = (double *)(ws + l.squares);
     uint16_t *x[2] = {(uint16_t *)(ws + l.x0), (uint16_t *)(ws + l.x1)}, *a = (uint16_t *)(ws + l.a), *b = (uint16_t *)(ws + l.b);
-    float *last = (float *)(ws + l.last);
-    const int transposed = rows > cols;
     const double s = std::exp2(std::nearbyint(0.5 * std::log2((double)l.n)));
     const auto ok = [] { return hipGetLastError() == hipSuccess; };
 
     const OrthoMomentum mom{velocity, g8, rows * cols, inv_loss_scale, momentum, nesterov, l.blocks, skip_if_nonzero, squares, stats};
     hipLaunchKernelGGL(ortho_momentum_kernel, dim3((unsigned)l.blocks, (unsigned)batch), dim3(256), 0, st, mom);
     if (!ok()) return MP8_ERR_HIP;
-    const OrthoStart start{velocity, g8, (int)rows, (int)cols, transposed, inv_loss_scale, momentum, nesterov, l.blocks, squares, skip_if_nonzero,
-                           s, x[0], l.ld, l.m8 * l.ld, (int)l.m8};
-    hipLaunchKernelGGL(ortho_start_kernel, dim3((unsigned)(l.ld / 64), (unsigned)(l.lda / 64), (unsigned)batch), dim3(256), 0, st, start);
+    const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = rows * l.ld, ab = l.m * l.lda;
+    const OrthoStart start{velocity, g8, (int)rows, (int)cols, inv_loss_scale, momentum, nesterov, l.blocks, squares, skip_if_nonzero, s, x[0], l.ld, xb,
+                           make_fastdiv((uint32_t)(c8 / 8))};
+    const int64_t blocks = up(rows * (c8 / 8), 256) / 256;
+    hipLaunchKernelGGL(ortho_start_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)batch), dim3(256), 0, st, start);
     if (!ok()) return MP8_ERR_HIP;
-    const int64_t xb = l.m8 * l.ld, ab = l.m8 * l.lda;
+    const OrthoOperand A{a, l.lda, ab}, P{b, l.lda, ab};
     for (int k = 0; k < steps; ++k) {
-        const uint16_t *now = x[k & 1];
-        const OrthoSymmetric gram{nullptr, a, l.lda, ab, (int)l.m8, 0.0f, (float)(kUp / (s * s))};
-        if (!ortho_product<false>(batch, now, l.ld, xb, now, l.ld, xb, l.m8, l.m8, l.n8, true, skip_if_nonzero, gram, st)) return MP8_ERR_HIP;
-        const OrthoSymmetric poly{a, b, l.lda, ab, (int)l.m8, kOrthoB, kOrthoC * kDown};
-        if (!ortho_product<false>(batch, a, l.lda, ab, a, l.lda, ab, l.m8, l.m8, l.m8, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
-        const OrthoNext next{now, k + 1 < steps ? x[(k + 1) & 1] : nullptr, last, l.ld, xb, (int)l.m8, (int)l.n8, (float)(1.0 / s)};
-        if (!ortho_product<true>(batch, b, l.lda, ab, now, l.ld, xb, l.m8, l.n8, l.m8, false, skip_if_nonzero, next, st)) return MP8_ERR_HIP;
+        const OrthoOperand X{x[k & 1], l.ld, xb};
+        const OrthoSymmetric gram{nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
+        if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
+                         : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))
+            return MP8_ERR_HIP;
+        const OrthoSymmetric poly{a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+        if (!ortho_product<false, false>(batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
+        auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
+            return rows <= cols ? ortho_product<false, true>(batch, P, X, rows, c8, l.m, false, skip_if_nonzero, epi, st)
+                                : ortho_product<false, false>(batch, X, P, rows, cols, l.m, false, skip_if_nonzero, epi, st);
+        };
+        const bool last = k + 1 == steps;
+        if (!last && !second(OrthoNext{X.p, x[(k + 1) & 1], l.ld, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
+        if (last && !second(OrthoUpdate{X.p, l.ld, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
+            return MP8_ERR_HIP;
     }
-    const OrthoApply apply{last, l.ld, xb, (int)rows, (int)cols, transposed, w16, w8_out, -lr, weight_decay, round == MP8_SR, seed, offset, skip_if_nonzero};
-    hipLaunchKernelGGL(ortho_apply_kernel, dim3((unsigned)((cols + 63) / 64), (unsigned)((rows + 63) / 64), (unsigned)batch), dim3(256), 0, st, apply);
-    return ok() ? MP8_OK : MP8_ERR_HIP;
+    return MP8_OK;
 }

@@ -165,10 +165,7 @@ __device__ __forceinline__ void xent_count_half(StatsAcc &st, float y) {
     st.zero_codes += (h & 0x7FFFu) == 0u ? 1u : 0u;
 }
 
-// A gradient, complete in its tile: unscaled, rounded and stored.  Rows of whole groups of eight.  FULL: with codes and statistics, which
-// take more code and registers than fit beside the accumulators of a 256x256 tile (they went to memory: 8192 x 131072 x 2048 six
-// times as long); its callers take 128x128 tiles then.
-template <bool FULL>
+// A gradient, complete in its tile: unscaled, rounded and stored.  Rows of whole groups of eight.
 struct XentOut {
     const int *exponent;
     float scale;
@@ -184,53 +181,30 @@ struct XentOut {
         const float unscale = ldexpf(scale, *exponent - kErrorExponent);
         const Philox rng(seed, offset);
         StatsAcc st;
-        const uint32_t seen = FULL && stats != nullptr ? StatsAcc::peek(stats) : 0u;
-        const int h = at.lane >> 5;
+        const uint32_t seen = stats != nullptr ? StatsAcc::peek(stats) : 0u;
+        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+            if (r >= rows || c >= cols) return;
+            float v[8];
 #pragma unroll
-        for (int i = 0; i < T::MT; ++i) {
-            const int r = at.row(i);
-#pragma unroll
-            for (int j = 0; j < T::NT; ++j) {
-                if (at.col0 + 32 * j >= cols) break;
-#pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = acc[i][j][4 * g + e] * unscale;
-                    // before the half waves exchange: columns 8 g + 4 h .. and eight further; after it: eight from 8 (g + h) on
-                    const int c = at.col0 + 32 * j + 8 * g, mine = c + 8 * h;
-                    const int64_t first = (row0 + r) * (int64_t)cols + c;
-                    const bool in0 = r < rows && c < cols, in1 = r < rows && c + 8 < cols, in = h ? in1 : in0;
-                    if (!FULL || out16 != nullptr) {
-                        const u32x4 o = half_pack16(v);
-                        if (in) *reinterpret_cast<u32x4 *>(out16 + first + mine - c) = o;
-                    }
-                    if (FULL && out8 != nullptr) {
-                        Words4 w0 = {0, 0}, w1 = {0, 0};
-                        if (sr) {  // each half wave makes one of the two blocks and hands over the half it does not need
-                            const uint4 b = rng.block((uint64_t)(first + 8 * h) >> 3);
-                            const auto s01 = __builtin_amdgcn_permlane32_swap(b.x, b.z, false, false);
-                            const auto s23 = __builtin_amdgcn_permlane32_swap(b.y, b.w, false, false);
-                            w0 = {s01[0], s23[0]};
-                            w1 = {s01[1], s23[1]};
-                        }
-                        const uint32_t p0 = e5m2_pack4_rt(v, w0.r01, w0.r23, sr != 0, sat != 0), p1 = e5m2_pack4_rt(v + 4, w1.r01, w1.r23, sr != 0, sat != 0);
-                        if (stats != nullptr) {
-                            if (in0) st.add4(v, p0);
-                            if (in1) st.add4(v + 4, p1);
-                        }
-                        const auto s = __builtin_amdgcn_permlane32_swap(p0, p1, false, false);
-                        const u32x2 o = {s[0], s[1]};
-                        if (in) *reinterpret_cast<u32x2 *>(out8 + first + mine - c) = o;
-                    } else if (FULL && stats != nullptr) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (e < 4 ? in0 : in1) xent_count_half(st, v[e]);
-                    }
+            for (int e = 0; e < 8; ++e) v[e] = sum[e] * unscale;
+            const int64_t i = (row0 + r) * (int64_t)cols + c;
+            if (out16 != nullptr) *reinterpret_cast<u32x4 *>(out16 + i) = half_round8(v);
+            if (out8 != nullptr) {
+                uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                if (sr) w = rng.block((uint64_t)i >> 3);
+                const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+                const u32x2 o = {e5m2_pack4_rt(lo, w.x, w.y, sr != 0, sat != 0), e5m2_pack4_rt(hi, w.z, w.w, sr != 0, sat != 0)};
+                *reinterpret_cast<u32x2 *>(out8 + i) = o;
+                if (stats != nullptr) {
+                    st.add4(lo, o.x);
+                    st.add4(hi, o.y);
                 }
+            } else if (stats != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xent_count_half(st, v[e]);
             }
-        }
-        if (FULL && stats != nullptr) st.flush(stats, seen);
+        });
+        if (stats != nullptr) st.flush(stats, seen);
     }
 };
 
@@ -527,6 +501,7 @@ bool product(int tile, const void *a, int64_t lda, const void *b, int64_t ldb, i
              const Epi &epi, hipStream_t stream) {
     const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows, cols, kc, tile, tile, splits, false);
     if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, 1, epi, stream);
+    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, 1, epi, stream);
     if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, 1, epi, stream);
     return half_gemm_launch<Half64, ATN, BTN>(p, 1, epi, stream);
 }
@@ -647,15 +622,8 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     auto direct = [&](auto atn, int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
                       uint8_t *out8, uint64_t offset, mp8_stats *stats) {
         constexpr bool ATN = decltype(atn)::value;
-        const int64_t rows_a = ATN ? up(rows, 8) : rows;
-        auto epi = [&](auto full) {
-            return XentOut<decltype(full)::value>{exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0,
-                                                  seed, offset, stats};
-        };
-        if (out8 == nullptr && stats == nullptr) return product<true, ATN>(tile, a, lda, b, ldb, rows_a, K8, kc, 1, epi(std::false_type{}), st);
-        const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows_a, K8, kc, tile == 64 ? 64 : 128, tile == 64 ? 64 : 128, 1, false);
-        return tile == 64 ? half_gemm_launch<Half64, ATN, true>(p, 1, epi(std::true_type{}), st)
-                          : half_gemm_launch<Half128, ATN, true>(p, 1, epi(std::true_type{}), st);
+        const XentOut epi{exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0, seed, offset, stats};
+        return product<true, ATN>(tile, a, lda, b, ldb, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
     };
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
