@@ -144,6 +144,8 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         r = origin + r < extent ? r : extent - 1 - origin;
         return (uint32_t)(r * ld) + 16 * lchunk;
     };
+    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane, lds};
+    auto ahead = epi.ahead(at);  // what the epilogue wants to have read by then
     uint32_t oa[A_DMA], ob[B_DMA];
 #pragma unroll
     for (int q = 0; q < A_DMA; ++q) oa[q] = offset(ATN, q, row0, p.rows, p.lda);
@@ -283,8 +285,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
             }
         }
     }
-    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane, lds};
-    epi(at, acc);
+    epi(at, acc, ahead);
 }
 
 // Sixteen columns of accumulator elements 4 g .. 4 g + 7 (g even), packed as halves: the lower half wave ends up with columns
@@ -298,18 +299,20 @@ __device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
     return u32x4{s0[0], s1[0], s0[1], s1[1]};
 }
 
-// f(r, c, v) for every eight neighbouring columns c .. c+7 of rows r of the wave's part: bands of 32 rows pass through LDS (a
-// region of the ring per wave), so that f's code is there once per band, and the lanes that share a row lie side by side: stores
-// and loads of whole 128-byte lines.  before(i, band): called when
-// the i-th one lies in LDS, 32 rows of PITCH floats.
+// f(r, c, v, x) for every eight neighbouring columns c .. c+7 of rows r of the wave's part, x = load(r, c): bands of 32 rows pass through
+// LDS (a region of the ring per wave), so that the lanes that share a row lie side by side and store and load whole 128-byte lines, and
+// that f's code is there MOST_U times per band and not once per eight accumulators; as many loads are under way together.  before(i, band):
+// called when the i-th band lies in LDS, 32 rows of kHalfBandPitch floats.
 template <class T>
 constexpr int kHalfBandPitch = T::WTN + 4;
-template <class T, class F, class Between>
-__device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f, const Between &before) {
+template <int MOST_U = 4, class T, class Load, class F, class Before>
+__device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Load &load, const F &f, const Before &before) {
     constexpr int PITCH = kHalfBandPitch<T>, PER = T::WTN / 8, ROWS = 64 / PER;  // lanes of a row, rows of a pass (192: 5 rows, 60 lanes)
+    constexpr int PASSES = (32 + ROWS - 1) / ROWS, U = PASSES < MOST_U ? PASSES : MOST_U;
     static_assert(4 * 32 * PITCH * 4 <= T::NSTAGE * (T::BM + T::BN) * 128, "the bands fit the ring");
     float *band = reinterpret_cast<float *>(at.lds) + at.wave * 32 * PITCH;
     const int lr = at.lane / PER, lc = 8 * (at.lane % PER);
+    const bool lane_used = 64 % PER == 0 || lr < ROWS;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < T::MT; ++i) {
@@ -320,19 +323,31 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
                 const f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
                 *reinterpret_cast<f32x4 *>(band + (at.lane & 31) * PITCH + 32 * j + 8 * g + 4 * (at.lane >> 5)) = v;
             }
-        before(i, band);
+        const int r0 = at.row0 + 32 * i, c = at.col0 + lc;
 #pragma unroll 1
-        for (int k = lr; k < 32; k += ROWS) {
-            if (64 % PER != 0 && lr >= ROWS) break;
-            const f32x4 lo = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc), hi = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc + 4);
-            const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            f(at.row0 + 32 * i + k, at.col0 + lc, v);
+        for (int q = 0; q < PASSES; q += U) {
+            decltype(load(0, 0)) x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = lr + (q + u) * ROWS;
+                if (lane_used && k < 32) x[u] = load(r0 + k, c);
+            }
+            if (q == 0) before(i, band);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = lr + (q + u) * ROWS;
+                if (!lane_used || k >= 32) continue;
+                const f32x4 lo = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc), hi = *reinterpret_cast<const f32x4 *>(band + k * PITCH + lc + 4);
+                const float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+                f(r0 + k, c, v, x[u]);
+            }
         }
     }
 }
+struct HalfNothing {};
 template <class T, class F>
 __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f) {
-    half_bands(at, acc, f, [](int, float *) {});
+    half_bands(at, acc, [](int, int) { return HalfNothing{}; }, [&](int r, int c, const float (&v)[8], HalfNothing) { f(r, c, v); }, [](int, float *) {});
 }
 
 // Eight halves from eight FP32 values, to nearest.
@@ -343,26 +358,36 @@ __device__ __forceinline__ u32x4 half_round8(const float v[8]) {
     return w;
 }
 
+struct HalfNoneAhead {
+    template <class P>
+    __device__ __forceinline__ HalfNothing ahead(const P &) const { return {}; }
+};
+
 // The FP32 tile itself, scaled by nothing, stored or added to what is there: slab `split` of [rows, ld] floats (ld a multiple of
 // eight and at least the columns, so that whole groups of eight may be stored).
-struct HalfEpiSum {
+struct HalfEpiSum : HalfNoneAhead {
     float *out;
     int64_t ld, slab, batch;  // in floats
     int rows, cols, add;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
         float *base = out + at.batch * batch + at.split * slab;
-        half_bands(at, acc, [&](int r, int c, const float (&v)[8]) {
+        struct Eight {
+            f32x4 lo, hi;
+        };
+        half_bands(at, acc, [&](int r, int c) {
+            Eight x{};
+            if (add && r < rows && c < cols) {
+                x.lo = *reinterpret_cast<const f32x4 *>(base + r * ld + c);
+                x.hi = *reinterpret_cast<const f32x4 *>(base + r * ld + c + 4);
+            }
+            return x;
+        }, [&](int r, int c, const float (&v)[8], const Eight &x) {
             if (r >= rows || c >= cols) return;
             f32x4 *to = reinterpret_cast<f32x4 *>(base + r * ld + c);
-            f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
-            if (add) {
-                lo += to[0];
-                hi += to[1];
-            }
-            to[0] = lo;
-            to[1] = hi;
-        });
+            to[0] = x.lo + f32x4{v[0], v[1], v[2], v[3]};
+            to[1] = x.hi + f32x4{v[4], v[5], v[6], v[7]};
+        }, [](int, float *) {});
     }
 };
 

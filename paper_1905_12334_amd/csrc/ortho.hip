@@ -25,37 +25,46 @@ constexpr float kUp = 16384.0f, kDown = 1.0f / 16384.0f;  // the scale of A and 
 
 // A symmetric output of halves, made from its upper tiles: v = linear * in[r, c] + scale * acc at (r, c) and, off the diagonal's
 // tiles, at (c, r), turned round by the lanes that read the band.  Columns m .. m8 - 1 are zero.
-struct OrthoSymmetric {
+struct OrthoSymmetric : HalfNoneAhead {
     const uint16_t *in;  // nullable
     uint16_t *out;
     int64_t ld, batch;   // in halves
     int m;
     float linear, scale;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
         const uint16_t *x = in != nullptr ? in + at.batch * batch : nullptr;
         uint16_t *o = out + at.batch * batch;
         const bool mirror = at.tm != at.tn;
-        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
-            if (r >= m || c >= m) return;
+        half_bands(at, acc, [&](int r, int c) {
             u32x4 xw = {0, 0, 0, 0};
-            if (x != nullptr) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
-            *reinterpret_cast<u32x4 *>(o + r * ld + c) = value(xw, sum, m - c);
+            if (x != nullptr && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
+            return xw;
+        }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
+            if (r < m && c < m) *reinterpret_cast<u32x4 *>(o + r * ld + c) = value(xw, sum, m - c);
         }, [&](int i, const float *band) {
             if (!mirror) return;
             // four lanes per row of the turned band: its rows are the band's columns, its columns rows of the tile, all of which exist
             // (a tile below the diagonal's ends at a tile border)
             const int k = 8 * (at.lane & 3), r = at.row0 + 32 * i + k;
+            constexpr int U = T::WTN / 16 < 4 ? T::WTN / 16 : T::WTN % 64 == 0 ? 4 : 3;
 #pragma unroll 1
-            for (int n = at.lane >> 2; n < T::WTN; n += 16) {
-                const int c = at.col0 + n;
-                if (c >= m) break;
-                float sum[8];
+            for (int n0 = at.lane >> 2; n0 < T::WTN; n0 += 16 * U) {
+                u32x4 xw[U];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
-                u32x4 xw = {0, 0, 0, 0};
-                if (x != nullptr) xw = *reinterpret_cast<const u32x4 *>(x + c * ld + r);
-                *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw, sum, 8);
+                for (int u = 0; u < U; ++u) {
+                    const int c = at.col0 + n0 + 16 * u;
+                    xw[u] = u32x4{0, 0, 0, 0};
+                    if (x != nullptr && c < m) xw[u] = *reinterpret_cast<const u32x4 *>(x + c * ld + r);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int n = n0 + 16 * u, c = at.col0 + n;
+                    float sum[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
+                    if (c < m) *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw[u], sum, 8);
+                }
             }
         });
     }
@@ -71,27 +80,30 @@ struct OrthoSymmetric {
 };
 
 // The next iterate, a X + scale * acc, as halves.  Columns up to the next multiple of eight are stored (they are zero).
-struct OrthoNext {
+struct OrthoNext : HalfNoneAhead {
     const uint16_t *x;
     uint16_t *out;
     int64_t ld, batch; // in halves
     int rows, cols;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
-        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
+        const int64_t base = at.batch * batch;
+        half_bands(at, acc, [&](int r, int c) {
+            u32x4 xw = {0, 0, 0, 0};
+            if (r < rows && c < cols) xw = *reinterpret_cast<const u32x4 *>(x + base + r * ld + c);
+            return xw;
+        }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
             if (r >= rows || c >= cols) return;
-            const int64_t i0 = at.batch * batch + r * ld + c;
-            const u32x4 xw = *reinterpret_cast<const u32x4 *>(x + i0);
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(kOrthoA, half_bits_to_f32(xw[e >> 1] >> (16 * (e & 1))), kDown * sum[e]);
-            *reinterpret_cast<u32x4 *>(out + i0) = half_round8(v);
-        });
+            *reinterpret_cast<u32x4 *>(out + base + r * ld + c) = half_round8(v);
+        }, [](int, float *) {});
     }
 };
 
 // The last iterate goes straight into the weights: w' = w - lr (X + wd w), rounded to half, and its 8-bit copy.
-struct OrthoUpdate {
+struct OrthoUpdate : HalfNoneAhead {
     const uint16_t *x;
     int64_t ld, batch;
     int rows, cols;
@@ -101,23 +113,32 @@ struct OrthoUpdate {
     int sr;
     uint64_t seed, offset;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
         const Philox rng(seed, offset);
         const bool whole = (cols & 7) == 0;
         const int64_t first = (int64_t)at.batch * rows * cols;
-        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
-            if (r >= rows || c >= cols) return;
-            const u32x4 xw = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + r * ld + c);
+        struct Eight {
+            u32x4 x, w;
+        };
+        // (four copies of this code per band are too much for the compiler where there are three or four bands)
+        half_bands<(T::BM > 128 ? 1 : 4)>(at, acc, [&](int r, int c) {
+            Eight in{};
+            if (r >= rows || c >= cols) return in;
+            in.x = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + r * ld + c);
             const int64_t i0 = first + (int64_t)r * cols + c;
-            const int n = cols - c < 8 ? cols - c : 8;
-            u32x4 ww = {0, 0, 0, 0};
             if (whole) {
-                ww = *reinterpret_cast<const u32x4 *>(w16 + i0);
+                in.w = *reinterpret_cast<const u32x4 *>(w16 + i0);
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (e < n) ww[e >> 1] |= (uint32_t)w16[i0 + e] << (16 * (e & 1));
+                    if (c + e < cols) in.w[e >> 1] |= (uint32_t)w16[i0 + e] << (16 * (e & 1));
             }
+            return in;
+        }, [&](int r, int c, const float (&sum)[8], const Eight &in) {
+            if (r >= rows || c >= cols) return;
+            const int64_t i0 = first + (int64_t)r * cols + c;
+            const int n = cols - c < 8 ? cols - c : 8;
+            const u32x4 xw = in.x, ww = in.w;
             uint32_t rw[4] = {0, 0, 0, 0};
             if (sr) {
                 if (whole) {
@@ -155,7 +176,7 @@ struct OrthoUpdate {
                         if (w8 != nullptr) w8[i0 + e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
                     }
             }
-        });
+        }, [](int, float *) {});
     }
 };
 
@@ -393,19 +414,19 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const OrthoOperand A{a, l.lda, ab}, P{b, l.lda, ab};
     for (int k = 0; k < steps; ++k) {
         const OrthoOperand X{x[k & 1], l.ld, xb};
-        const OrthoSymmetric gram{nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
+        const OrthoSymmetric gram{{}, nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
         if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
                          : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))
             return MP8_ERR_HIP;
-        const OrthoSymmetric poly{a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+        const OrthoSymmetric poly{{}, a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
         if (!ortho_product<false, false>(batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
         auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
             return rows <= cols ? ortho_product<false, true>(batch, P, X, rows, c8, l.m, false, skip_if_nonzero, epi, st)
                                 : ortho_product<false, false>(batch, X, P, rows, cols, l.m, false, skip_if_nonzero, epi, st);
         };
         const bool last = k + 1 == steps;
-        if (!last && !second(OrthoNext{X.p, x[(k + 1) & 1], l.ld, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
-        if (last && !second(OrthoUpdate{X.p, l.ld, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
+        if (!last && !second(OrthoNext{{}, X.p, x[(k + 1) & 1], l.ld, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
+        if (last && !second(OrthoUpdate{{}, X.p, l.ld, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
             return MP8_ERR_HIP;
     }
     return MP8_OK;

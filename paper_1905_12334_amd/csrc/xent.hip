@@ -33,19 +33,34 @@ __device__ __forceinline__ void xent_join(f32x2 &t, f32x2 p) {
     t = f32x2{b, s0 + s1};
 }
 
+// Column of a target among a wave's, the first of which is class `first`; -1 if it is none of them (`left`: that exist).
+template <class T>
+__device__ __forceinline__ int xent_column(int64_t target, int64_t first, int left) {
+    const int64_t rel = target - first;
+    return rel >= 0 && rel < T::WTN && rel < left ? (int)rel : -1;
+}
+
 struct XentStats {
     const int64_t *targets;
     f32x2 *part;     // [parts, M]: (B, sum) of the columns of one tile, without the target
     float *z_target; // [M]
     int M, N, first; // `first`: class of this piece's column 0
     int part0;       // of this piece
+    template <int MT>
+    struct Ahead {
+        int target[MT];  // of the wave's columns, or -1
+    };
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
-        const int h4 = 4 * (at.lane >> 5), left = N - at.col0;  // columns of this wave's tile that exist
-        int64_t target[T::MT];
-        f32x2 mine[T::MT];
+    __device__ __forceinline__ Ahead<T::MT> ahead(const HalfPlace<T> &at) const {
+        Ahead<T::MT> a;
 #pragma unroll
-        for (int i = 0; i < T::MT; ++i) target[i] = at.row(i) < M ? targets[at.row(i)] : -1;
+        for (int i = 0; i < T::MT; ++i) a.target[i] = at.row(i) < M ? xent_column<T>(targets[at.row(i)], first + at.col0, N - at.col0) : -1;
+        return a;
+    }
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Ahead<T::MT> &a) const {
+        const int h4 = 4 * (at.lane >> 5), left = N - at.col0;  // columns of this wave's tile that exist
+        f32x2 mine[T::MT];
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) {
             f32x16 (&z)[T::NT] = acc[i];
@@ -56,10 +71,8 @@ struct XentStats {
                     for (int e = 0; e < 16; ++e)
                         if (32 * j + 8 * (e >> 2) + h4 + (e & 3) >= left) z[j][e] = -__builtin_inff();
             }
-            const int64_t rel = target[i] - first - at.col0;
-            const bool here = rel >= 0 && rel < T::WTN && rel < left;
-            if (__builtin_amdgcn_ballot_w64(here) != 0) {
-                const int c = here ? (int)rel - h4 : -1;
+            if (__builtin_amdgcn_ballot_w64(a.target[i] >= 0) != 0) {
+                const int c = a.target[i] - h4;  // (-1 - 4 h meets no column)
 #pragma unroll
                 for (int j = 0; j < T::NT; ++j)
 #pragma unroll
@@ -111,22 +124,37 @@ struct XentError {
     uint16_t *out;                     // [M, ld]
     int64_t ld;
     int M, N, first;                   // N: columns that exist; those behind them, to the tile's end, become zero
+    template <int MT>
+    struct Ahead {
+        float factor[MT], base[MT], at_target[MT];  // of the rows; what e is at the target, without the factor
+        int target[MT];
+    };
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
-        const int h4 = 4 * (at.lane >> 5);
+    __device__ __forceinline__ Ahead<T::MT> ahead(const HalfPlace<T> &at) const {
+        Ahead<T::MT> a;
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) {
             const int r = at.row(i);
             const bool row = r < M;
-            const float f = row ? factor[r] : 0.0f;
-            const float base = row ? lse[r] * kLog2e : 0.0f;
-            const int64_t rel = row ? targets[r] - first - at.col0 : -1;
-            const bool here = rel >= 0 && rel < T::WTN;
-            const bool any = __builtin_amdgcn_ballot_w64(here) != 0;
-            const int c = here ? (int)rel - h4 : -1;
+            a.factor[i] = row ? factor[r] : 0.0f;
+            a.base[i] = row ? lse[r] : 0.0f;
+            a.at_target[i] = row ? loss[r] : 0.0f;
+            a.target[i] = row ? xent_column<T>(targets[r], first + at.col0, N - at.col0) : -1;
+        }
+        return a;
+    }
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Ahead<T::MT> &a) const {
+        const int h4 = 4 * (at.lane >> 5), left = N - at.col0;
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            const int r = at.row(i);
+            const bool row = r < M;
+            const float f = a.factor[i], base = a.base[i] * kLog2e;
+            const bool any = __builtin_amdgcn_ballot_w64(a.target[i] >= 0) != 0;
+            const int c = a.target[i] - h4;  // (-1 - 4 h meets no column)
             // exp(-loss) - 1: the target's probability is one less what the others have, to the loss's precision
-            const float e_target = any && here ? f * expm1f(-loss[r]) : 0.0f;
-            const int left = N - at.col0;
+            const float e_target = any ? f * expm1f(-a.at_target[i]) : 0.0f;
 #pragma unroll
             for (int j = 0; j < T::NT; ++j) {
                 if (at.col0 + 32 * j >= ld) break;
@@ -166,7 +194,7 @@ __device__ __forceinline__ void xent_count_half(StatsAcc &st, float y) {
 }
 
 // A gradient, complete in its tile: unscaled, rounded and stored.  Rows of whole groups of eight.
-struct XentOut {
+struct XentOut : HalfNoneAhead {
     const int *exponent;
     float scale;
     int rows, cols;
@@ -177,7 +205,7 @@ struct XentOut {
     uint64_t seed, offset;
     mp8_stats *stats;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT]) const {
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
         const float unscale = ldexpf(scale, *exponent - kErrorExponent);
         const Philox rng(seed, offset);
         StatsAcc st;
@@ -421,7 +449,8 @@ struct Layout {
     size_t factor, exponent, e, dx, dw, total;  // backward: (copies as above,) the tokens' factors, e, FP32 sums
 };
 // The logits' tiles: their epilogues take longer than others, and two workgroups per CU hide them behind each other's products.  Measured,
-// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 215 / 174, 1021 x 32003 x 1000 90 / 78, 8192 x 131072 x 2048 4060 / 4540.
+// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 215 / 174, 1021 x 32003 x 1000 90 / 78, 6007 x 37003 x 1000 598 / 630,
+// 8192 x 131072 x 2048 4060 / 4540.
 HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
     HalfPlan best = half_plan(1, M, cols, K, false, 1);
     if (best.tile == 64) return best;
@@ -429,7 +458,7 @@ HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
     for (const int tile : {256, 128}) {
         const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 12.0 : 4.5;
         const double rounds = std::ceil((double)(((M + tile - 1) / tile) * ((cols + tile - 1) / tile)) / slots);
-        const double t = rounds * ((double)((K + 63) / 64) * (tile == 256 ? 1.73 : 0.93) + epilogue);
+        const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.73 : 1.03) + (rounds + 1.0) * epilogue;
         if (t < least) {
             least = t;
             best.tile = tile;
@@ -622,7 +651,7 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     auto direct = [&](auto atn, int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
                       uint8_t *out8, uint64_t offset, mp8_stats *stats) {
         constexpr bool ATN = decltype(atn)::value;
-        const XentOut epi{exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0, seed, offset, stats};
+        const XentOut epi{{}, exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0, seed, offset, stats};
         return product<true, ATN>(tile, a, lda, b, ldb, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
     };
     for (int64_t c = 0; c < N; c += s.piece) {
@@ -640,7 +669,7 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
             if (plans.dx_direct) {
                 if (!direct(std::false_type{}, plans.dx.tile, e, lde, wp, ld_w, M, cols, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
             } else {
-                const HalfEpiSum sum{dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
+                const HalfEpiSum sum{{}, dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
                 if (!product<true, false>(plans.dx.tile, e, lde, wp, ld_w, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
             }
         }
@@ -648,7 +677,7 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
             if (plans.dw_direct) {
                 if (!direct(std::true_type{}, plans.dw.tile, e, lde, xs, s.Kp, cols, M, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             } else {
-                const HalfEpiSum sum{dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
+                const HalfEpiSum sum{{}, dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
                 if (!product<true, true>(plans.dw.tile, e, lde, xs, s.Kp, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
                 if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             }
