@@ -67,17 +67,20 @@ __device__ __forceinline__ HalfTile half_tile(const HalfGemm &p) {
     return t;
 }
 
-// Tiles: four waves, WGM x WGN of them, each with a grid of 32x32 accumulators.  WHOLE: how far ahead fragments are fetched, see the kernel.
-template <int BM_, int BN_, int NSTAGE_, int MINBLOCKS_, bool WHOLE_>
+// Tiles of four waves; their schedules are described at the kernel.  WGM x WGN waves have a part of the tile each, a grid of 32x32
+// accumulators (kByIndex: when the sums are complete).
+enum HalfSchedule { kAhead, kWhole, kByIndex };
+template <int BM_, int BN_, int NSTAGE_, int MINBLOCKS_, HalfSchedule SCHEDULE_>
 struct HalfTiling {
     static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = 2, NSTAGE = NSTAGE_, MINBLOCKS = MINBLOCKS_;
     static constexpr int WTM = BM / WGM, WTN = BN / WGN, MT = WTM / 32, NT = WTN / 32;
-    static constexpr bool WHOLE = WHOLE_;
+    static constexpr HalfSchedule SCHEDULE = SCHEDULE_;
 };
-using Half256 = HalfTiling<256, 256, 2, 1, false>;
-using Half192 = HalfTiling<192, 192, 2, 1, false>;
-using Half128 = HalfTiling<128, 128, 2, 2, true>;
-using Half64 = HalfTiling<64, 64, 4, 2, true>;
+using Half256 = HalfTiling<256, 256, 2, 1, kAhead>;
+using Half192 = HalfTiling<192, 192, 2, 1, kAhead>;
+using Half128 = HalfTiling<128, 128, 2, 2, kWhole>;
+using Half64 = HalfTiling<64, 64, 4, 2, kWhole>;
+using Half64Few = HalfTiling<64, 64, 8, 1, kByIndex>;  // up to one per CU
 using f32x2 = float __attribute__((ext_vector_type(2)));
 
 // Where a lane's accumulators lie.  Element e of accumulator (i, j) is row row(i), column col(j) + 8 (e / 4) + e % 4.
@@ -92,11 +95,13 @@ struct HalfPlace {
 };
 
 // Operands pass through a ring of 128-byte-wide slabs in LDS, filled by direct-to-LDS loads, a stage (64 contraction indices)
-// being four sub-steps of sixteen.  Two schedules:
-//   one wave per SIMD (256x256): as in gemm_mfma_kernel, fragments are fetched one sub-step ahead, everything stands between two
+// being four sub-steps of sixteen.  Three schedules:
+//   kAhead (one wave per SIMD): as in gemm_mfma_kernel, fragments are fetched one sub-step ahead, everything stands between two
 //     matrix instructions, and the barrier stands behind the third sub-step, by which all fragments of the stage have been read
-//   WHOLE (two workgroups per CU): behind the barrier all fragments of the next stage are requested, then the loads of the stage that
+//   kWhole (two workgroups per CU): behind the barrier all fragments of the next stage are requested, then the loads of the stage that
 //     takes the place of the current one, then the current stage is multiplied; the other workgroup fills what is left
+//   kByIndex (few tiles, long contractions): the same, but each wave multiplies the whole tile over one of the four sub-steps, so that no
+//     fragment is read from LDS twice, and the waves' sums are added up at the end; a ring of eight stages
 // Gaussian operands, contraction 4096, TFLOP/s: 4096 x 4096 in 256x256 tiles 1090, in 128x128 tiles 1015 (with the other schedule 915), in
 // 64x64 tiles 570.  What bounds them: the 256x256 tile the power such data draws (all ones: 1390) and the clock it leaves
 // (1.85 GHz, 59 % of the cycles with a matrix instruction; loads that always hit, 1550), the small ones what a CU gets from L2 (14 TB/s in
@@ -168,16 +173,15 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         for (int q = 0; q < B_DMA; ++q) dma16_or_zero(bk, ob[q], inside(BTN, q), at + A_BYTES + q * 4096);
     };
 
-    // Fragment f of sub-step `sub`: lane l holds contraction indices 16 sub + 8 (l / 32) .. +7 of tile row l % 32 of
-    // A tile f (f < MT) or B tile f - MT.
+    // The fragment of A (or B) tile rows m .. m + 31 for sub-step `sub`: lane l holds contraction indices 16 sub + 8 (l / 32) .. +7 of row
+    // m + l % 32.
     const int frow = lane & 31, fk = lane >> 5, fsw = (frow >> 1) & 7, t16 = lane & 15;
     const int kt = 8 * fk + (t16 >> 2);                                  // transposing reads: this lane's contraction row
     const int ct = ((lane >> 4) & 1) * 2 + ((t16 & 3) >> 1);             // and chunk
     const int ft = kt * 128 + ((ct ^ (((t16 >> 3) & 1) << 2)) << 4) + 8 * (t16 & 1);
-    auto fragment = [&](int s, int sub, int f) -> half8 {
-        const uint8_t *slab = lds + (s % NSTAGE) * STAGE + (f < MT ? 0 : A_BYTES);
-        const int m = f < MT ? wm * WTM + 32 * f : wn * WTN + 32 * (f - MT);
-        if ((f < MT && ATN) || (f >= MT && BTN)) {
+    auto fragment_of = [&](int s, int sub, bool of_a, int m) -> half8 {
+        const uint8_t *slab = lds + (s % NSTAGE) * STAGE + (of_a ? 0 : A_BYTES);
+        if (of_a ? ATN : BTN) {
             using h4 = short __attribute__((ext_vector_type(4)));
             using lds_h4 = __attribute__((address_space(3))) h4;
             // (the panel's upper 32 tile rows are chunks 4 .. 7: the other value of the swizzled bit)
@@ -187,6 +191,8 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         }
         return *reinterpret_cast<const half8 *>(slab + (m + frow) * 128 + (((2 * sub + fk) ^ fsw) << 4));
     };
+    // fragment f of this wave's part: A tile f for f < MT, B tile f - MT otherwise
+    auto fragment = [&](int s, int sub, int f) { return f < MT ? fragment_of(s, sub, true, wm * WTM + 32 * f) : fragment_of(s, sub, false, wn * WTN + 32 * (f - MT)); };
     auto order = [&](int n) { return n == 0 ? MT : n == 1 ? 0 : n < NT + 1 ? MT + n - 1 : n - NT; };  // as first needed
 
     f32x16 acc[MT][NT];
@@ -218,7 +224,62 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         }
     wait_later((ks_count < NSTAGE ? ks_count : NSTAGE) - 1);
     __syncthreads();
-    if constexpr (T::WHOLE) {
+    if constexpr (T::SCHEDULE == kByIndex) {
+        constexpr int MK = BM / 32, NK = BN / 32;
+        static_assert(4 * MK * NK * 4096 <= NSTAGE * STAGE, "the waves' sums fit the ring");
+        f32x16 part[MK][NK] = {};
+        half8 fr[2][MK + NK];
+        auto read = [&](int s, half8 (&to)[MK + NK]) {
+#pragma unroll
+            for (int f = 0; f < MK + NK; ++f) to[f] = fragment_of(s, wave, f < MK, 32 * (f < MK ? f : f - MK));
+        };
+        auto stage = [&](int t, half8 (&now)[MK + NK], half8 (&then)[MK + NK]) {
+            if (t + 1 < ks_count) {
+                wait_stage(t + 1);
+                __syncthreads();  // the fragments of stage t have been read everywhere
+                read(t + 1, then);
+                if (t + NSTAGE < ks_count) {
+#pragma unroll
+                    for (int q = 0; q < G; ++q) issue_one(t + NSTAGE, q);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < MK; ++i)
+#pragma unroll
+                for (int j = 0; j < NK; ++j) part[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now[MK + j], now[i], part[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        read(0, fr[0]);
+        int t = 0;
+        for (; t + 1 < ks_count; t += 2) {
+            stage(t, fr[0], fr[1]);
+            stage(t + 1, fr[1], fr[0]);
+        }
+        if (t < ks_count) stage(t, fr[0], fr[1]);
+        __syncthreads();
+        f32x4 *sums = reinterpret_cast<f32x4 *>(lds);  // [wave][i][j][e / 4][lane]
+#pragma unroll
+        for (int i = 0; i < MK; ++i)
+#pragma unroll
+            for (int j = 0; j < NK; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    sums[(((wave * MK + i) * NK + j) * 4 + g) * 64 + lane] = f32x4{part[i][j][4 * g], part[i][j][4 * g + 1], part[i][j][4 * g + 2], part[i][j][4 * g + 3]};
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    f32x4 v = sums[((wm * MT + i) * NK + wn * NT + j) * 256 + g * 64 + lane];
+#pragma unroll
+                    for (int w = 1; w < 4; ++w) v += sums[(((w * MK + wm * MT + i) * NK + wn * NT + j) * 4 + g) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = v[e];
+                }
+    } else if constexpr (T::SCHEDULE == kWhole) {
         half8 fr[2][4][F];
         auto read = [&](int s, half8 (&to)[4][F]) {
 #pragma unroll
@@ -288,12 +349,18 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
     epi(at, acc, ahead);
 }
 
-// Sixteen columns of accumulator elements 4 g .. 4 g + 7 (g even), packed as halves: the lower half wave ends up with columns
+// Eight halves from eight FP32 values, to nearest: operands of further products, in which a NaN may have any payload.
+__device__ __forceinline__ u32x4 half_operand8(const float v[8]) {
+    half8 h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)v[e];
+    return __builtin_bit_cast(u32x4, h);
+}
+
+// Sixteen columns of accumulator elements 4 g .. 4 g + 7 (g even), packed as such halves: the lower half wave ends up with columns
 // 8 g .. +7 of the 32, the upper one with the eight after them, sixteen bytes each.
 __device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) w[q] = f16_from_f32<false>(v[2 * q], 0u) | f16_from_f32<false>(v[2 * q + 1], 0u) << 16;
+    const u32x4 w = half_operand8(v);
     const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
     const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
     return u32x4{s0[0], s1[0], s0[1], s1[1]};
@@ -350,7 +417,7 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
     half_bands(at, acc, [](int, int) { return HalfNothing{}; }, [&](int r, int c, const float (&v)[8], HalfNothing) { f(r, c, v); }, [](int, float *) {});
 }
 
-// Eight halves from eight FP32 values, to nearest.
+// Results: with the canonical NaN.
 __device__ __forceinline__ u32x4 half_round8(const float v[8]) {
     u32x4 w;
 #pragma unroll
@@ -403,7 +470,7 @@ struct HalfPlan {
 };
 
 // Estimated time, us, of `tiles` tiles over `stages` stages.  Measured (4096 x 4096 x 4096 and parts of it), us per stage: 64x64 tiles, up to 256
-// of them 0.25, 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93; 192x192, 64 0.81, 256 1.06; 256x256, 128 1.36, 256 1.73; more tiles
+// of them 0.26 (kByIndex 0.19), 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93; 192x192, 64 0.81, 256 1.06; 256x256, 128 1.36, 256 1.73; more tiles
 // take rounds.  On top come start and end of a workgroup.
 static inline double half_cost(int tile, int64_t tiles, double stages) {
     const int64_t slots = tile > 128 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
@@ -411,8 +478,11 @@ static inline double half_cost(int tile, int64_t tiles, double stages) {
     const double base = tile == 256 ? 10.0 : tile == 192 ? 8.0 : tile == 128 ? 5.0 : 3.5;
     const double rounds = (double)(full + (rest != 0)), over = (double)(rest - slots / 2) / (double)(slots / 2);
     const double part = rest == 0 ? 0.0 : over <= 0.0 ? half : half + over * (whole - half);
-    return base * (rounds < 1 ? 1 : 0.5 + 0.5 * rounds) + stages * ((double)full * whole + part);
+    const double t = base * (rounds < 1 ? 1 : 0.5 + 0.5 * rounds) + stages * ((double)full * whole + part), few = 4.4 + 0.19 * stages;
+    return tile == 64 && tiles <= 256 && few < t ? few : t;
 }
+// Few 64x64 tiles over a long contraction: kByIndex (the waves' sums cost 1 us, a stage 0.08 us less).
+static inline bool half_by_index(int64_t tiles, double stages) { return tiles <= 256 && stages >= 14; }
 
 // most_splits > 1: the slices' FP32 sums are written and added up by a pass of its own.
 static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int64_t kc, bool symmetric, int most_splits) {
@@ -468,6 +538,17 @@ static inline bool half_gemm_launch(const HalfGemm &p, int64_t batch, const Epi 
     const int64_t tiles = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
     hipLaunchKernelGGL((half_gemm_kernel<T, ATN, BTN, Epi>), dim3((unsigned)(tiles * p.splits * batch)), dim3(256), 0, stream, p, epi);
     return hipGetLastError() == hipSuccess;
+}
+
+// The tiles of a plan.
+template <bool ATN, bool BTN, class Epi>
+static inline bool half_gemm_launch_plan(int tile, const HalfGemm &p, int64_t batch, const Epi &epi, hipStream_t stream) {
+    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, batch, epi, stream);
+    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, batch, epi, stream);
+    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, batch, epi, stream);
+    const int64_t tiles = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
+    if (half_by_index(tiles * p.splits * batch, (double)p.ks_per)) return half_gemm_launch<Half64Few, ATN, BTN>(p, batch, epi, stream);
+    return half_gemm_launch<Half64, ATN, BTN>(p, batch, epi, stream);
 }
 
 }  // namespace mp8

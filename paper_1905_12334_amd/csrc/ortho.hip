@@ -23,25 +23,51 @@ namespace mp8 {
 constexpr float kOrthoA = 3.4445f, kOrthoB = -4.7750f, kOrthoC = 2.0315f;
 constexpr float kUp = 16384.0f, kDown = 1.0f / 16384.0f;  // the scale of A and of the polynomial
 
-// A symmetric output of halves, made from its upper tiles: v = linear * in[r, c] + scale * acc at (r, c) and, off the diagonal's
+// linear * x + scale * sum, as halves.
+__device__ __forceinline__ u32x4 ortho_combine(float linear, const u32x4 &x, float scale, const float (&sum)[8]) {
+    const half8 h = __builtin_bit_cast(half8, x);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(linear, (float)h[e], scale * sum[e]);
+    return half_operand8(v);
+}
+
+// A symmetric output of halves, made from its upper tiles: v = scale * acc (POLY: + linear * in[r, c]) at (r, c) and, off the diagonal's
 // tiles, at (c, r), turned round by the lanes that read the band.  Columns m .. m8 - 1 are zero.
+// With the conversions of the results' epilogues (canonical NaN, a test per element) two bands of a 128x128 tile took 5 us.
+template <bool POLY>
 struct OrthoSymmetric : HalfNoneAhead {
-    const uint16_t *in;  // nullable
+    const uint16_t *in;
     uint16_t *out;
     int64_t ld, batch;   // in halves
     int m;
     float linear, scale;
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
-        const uint16_t *x = in != nullptr ? in + at.batch * batch : nullptr;
+        const uint16_t *x = in + at.batch * batch;
         uint16_t *o = out + at.batch * batch;
         const bool mirror = at.tm != at.tn;
-        half_bands(at, acc, [&](int r, int c) {
+        auto load = [&](int r, int c) {
             u32x4 xw = {0, 0, 0, 0};
-            if (x != nullptr && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
+            if (POLY && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
             return xw;
-        }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
-            if (r < m && c < m) *reinterpret_cast<u32x4 *>(o + r * ld + c) = value(xw, sum, m - c);
+        };
+        auto value = [&](const u32x4 &xw, const float (&sum)[8]) {
+            if constexpr (POLY) return ortho_combine(linear, xw, scale, sum);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = scale * sum[e];
+            return half_operand8(v);
+        };
+        half_bands(at, acc, load, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
+            if (r >= m || c >= m) return;
+            u32x4 w = value(xw, sum);
+            if (m - c < 8) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e >= m - c) w[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
+            }
+            *reinterpret_cast<u32x4 *>(o + r * ld + c) = w;
         }, [&](int i, const float *band) {
             if (!mirror) return;
             // four lanes per row of the turned band: its rows are the band's columns, its columns rows of the tile, all of which exist
@@ -52,30 +78,17 @@ struct OrthoSymmetric : HalfNoneAhead {
             for (int n0 = at.lane >> 2; n0 < T::WTN; n0 += 16 * U) {
                 u32x4 xw[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int c = at.col0 + n0 + 16 * u;
-                    xw[u] = u32x4{0, 0, 0, 0};
-                    if (x != nullptr && c < m) xw[u] = *reinterpret_cast<const u32x4 *>(x + c * ld + r);
-                }
+                for (int u = 0; u < U; ++u) xw[u] = load(at.col0 + n0 + 16 * u, r);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int n = n0 + 16 * u, c = at.col0 + n;
                     float sum[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
-                    if (c < m) *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw[u], sum, 8);
+                    if (c < m) *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw[u], sum);
                 }
             }
         });
-    }
-    __device__ __forceinline__ u32x4 value(const u32x4 &xw, const float (&sum)[8], int left) const {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            v[e] = __builtin_fmaf(linear, half_bits_to_f32(xw[e >> 1] >> (16 * (e & 1))), scale * sum[e]);
-            if (e >= left) v[e] = 0.0f;
-        }
-        return half_round8(v);
     }
 };
 
@@ -94,10 +107,7 @@ struct OrthoNext : HalfNoneAhead {
             return xw;
         }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
             if (r >= rows || c >= cols) return;
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(kOrthoA, half_bits_to_f32(xw[e >> 1] >> (16 * (e & 1))), kDown * sum[e]);
-            *reinterpret_cast<u32x4 *>(out + base + r * ld + c) = half_round8(v);
+            *reinterpret_cast<u32x4 *>(out + base + r * ld + c) = ortho_combine(kOrthoA, xw, kDown, sum);
         }, [](int, float *) {});
     }
 };
@@ -363,10 +373,7 @@ bool ortho_product(int64_t batch, const OrthoOperand &a, const OrthoOperand &b, 
     const int tile = half_plan(batch, rows, cols, kc, symmetric, 1).tile;
     HalfGemm p = half_gemm_args(a.p, a.ld, a.batch, b.p, b.ld, b.batch, rows, cols, kc, tile, tile, 1, symmetric);
     p.skip = skip;
-    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, batch, epi, stream);
-    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, batch, epi, stream);
-    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, batch, epi, stream);
-    return half_gemm_launch<Half64, ATN, BTN>(p, batch, epi, stream);
+    return half_gemm_launch_plan<ATN, BTN>(tile, p, batch, epi, stream);
 }
 
 }  // namespace
@@ -414,11 +421,11 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const OrthoOperand A{a, l.lda, ab}, P{b, l.lda, ab};
     for (int k = 0; k < steps; ++k) {
         const OrthoOperand X{x[k & 1], l.ld, xb};
-        const OrthoSymmetric gram{{}, nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
+        const OrthoSymmetric<false> gram{{}, nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
         if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
                          : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))
             return MP8_ERR_HIP;
-        const OrthoSymmetric poly{{}, a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+        const OrthoSymmetric<true> poly{{}, a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
         if (!ortho_product<false, false>(batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
         auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
             return rows <= cols ? ortho_product<false, true>(batch, P, X, rows, c8, l.m, false, skip_if_nonzero, epi, st)

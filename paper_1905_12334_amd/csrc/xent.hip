@@ -529,10 +529,7 @@ template <bool BTN, bool ATN, class Epi>
 bool product(int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t cols, int64_t kc, int splits,
              const Epi &epi, hipStream_t stream) {
     const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows, cols, kc, tile, tile, splits, false);
-    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, 1, epi, stream);
-    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, 1, epi, stream);
-    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, 1, epi, stream);
-    return half_gemm_launch<Half64, ATN, BTN>(p, 1, epi, stream);
+    return half_gemm_launch_plan<ATN, BTN>(tile, p, 1, epi, stream);
 }
 
 bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t ld, int64_t rows, int64_t cols,
