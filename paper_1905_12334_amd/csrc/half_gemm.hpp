@@ -97,7 +97,8 @@ struct HalfPlace {
 // Operands pass through a ring of 128-byte-wide slabs in LDS, filled by direct-to-LDS loads, a stage (64 contraction indices)
 // being four sub-steps of sixteen.  Three schedules:
 //   kAhead (one wave per SIMD): as in gemm_mfma_kernel, fragments are fetched one sub-step ahead, everything stands between two
-//     matrix instructions, and the barrier stands behind the third sub-step, by which all fragments of the stage have been read
+//     matrix instructions, and the barrier stands behind the third sub-step, by which all fragments of the stage have been read;
+//     a's ring is one slab longer, all 160 KB of LDS at 256x256, so that its loads are spread over the stage
 //   kWhole (two workgroups per CU): behind the barrier all fragments of the next stage are requested, then the loads of the stage that
 //     takes the place of the current one, then the current stage is multiplied; the other workgroup fills what is left
 //   kByIndex (few tiles, long contractions): the same, but each wave multiplies the whole tile over one of the four sub-steps, so that no
@@ -119,7 +120,10 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
     constexpr int A_DMA = BM / 32, B_DMA = BN / 32, G = A_DMA + B_DMA;  // direct loads per wave and stage
     constexpr int F = MT + NT, NM = MT * NT;                             // fragments and matrix instructions per sub-step
     static_assert(G * (NSTAGE - 1) < 64, "vmcnt range");
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[NSTAGE * STAGE];
+    // kAhead: the ring of a has one slab more than that of b
+    constexpr bool AHEAD = T::SCHEDULE == kAhead;
+    constexpr int RING_A = (NSTAGE + 1) * A_BYTES;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[NSTAGE * STAGE + (AHEAD ? A_BYTES : 0)];
 
     if (p.skip != nullptr && *p.skip != 0u) return;
     const HalfTile tile = half_tile(p);
@@ -170,7 +174,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
         for (int q = 0; q < A_DMA; ++q) dma16_or_zero(ak, oa[q], inside(ATN, q), at + q * 4096);
 #pragma unroll
-        for (int q = 0; q < B_DMA; ++q) dma16_or_zero(bk, ob[q], inside(BTN, q), at + A_BYTES + q * 4096);
+        for (int q = 0; q < B_DMA; ++q) dma16_or_zero(bk, ob[q], inside(BTN, q), at + (AHEAD ? RING_A : A_BYTES) + q * 4096);
     };
 
     // The fragment of A (or B) tile rows m .. m + 31 for sub-step `sub`: lane l holds contraction indices 16 sub + 8 (l / 32) .. +7 of row
@@ -179,8 +183,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
     const int kt = 8 * fk + (t16 >> 2);                                  // transposing reads: this lane's contraction row
     const int ct = ((lane >> 4) & 1) * 2 + ((t16 & 3) >> 1);             // and chunk
     const int ft = kt * 128 + ((ct ^ (((t16 >> 3) & 1) << 2)) << 4) + 8 * (t16 & 1);
-    auto fragment_of = [&](int s, int sub, bool of_a, int m) -> half8 {
-        const uint8_t *slab = lds + (s % NSTAGE) * STAGE + (of_a ? 0 : A_BYTES);
+    auto fragment_at = [&](const uint8_t *slab, int sub, bool of_a, int m) -> half8 {
         if (of_a ? ATN : BTN) {
             using h4 = short __attribute__((ext_vector_type(4)));
             using lds_h4 = __attribute__((address_space(3))) h4;
@@ -191,6 +194,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         }
         return *reinterpret_cast<const half8 *>(slab + (m + frow) * 128 + (((2 * sub + fk) ^ fsw) << 4));
     };
+    auto fragment_of = [&](int s, int sub, bool of_a, int m) { return fragment_at(lds + (s % NSTAGE) * STAGE + (of_a ? 0 : A_BYTES), sub, of_a, m); };
     // fragment f of this wave's part: A tile f for f < MT, B tile f - MT otherwise
     auto fragment = [&](int s, int sub, int f) { return f < MT ? fragment_of(s, sub, true, wm * WTM + 32 * f) : fragment_of(s, sub, false, wn * WTN + 32 * (f - MT)); };
     auto order = [&](int n) { return n == 0 ? MT : n == 1 ? 0 : n < NT + 1 ? MT + n - 1 : n - NT; };  // as first needed
@@ -214,14 +218,31 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         const int later = ks_count - 1 - s;
         wait_later(later < NSTAGE - 2 ? later : NSTAGE - 2);
     };
+    // load q of a slab of a or b into LDS at `slot`
+    auto issue_a = [&](int s, int q, uint32_t slot) { dma16(a_tile + s * a_kstep, oa[q], lds0 + slot + wave * 1024 + q * 4096); };
+    auto issue_b = [&](int s, int q, uint32_t slot) { dma16(b_tile + s * b_kstep, ob[q], lds0 + RING_A + slot + wave * 1024 + q * 4096); };
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int s = 0; s < NSTAGE; ++s)
-        if (s < ks_count) {
-            if (s == 0 && has_tail && ks_begin == 0) issue_tail();
-            else
+        for (int s = 0; s < NSTAGE; ++s)
+            if (s < ks_count) {
+                if (s == 0 && has_tail && ks_begin == 0) issue_tail();
+                else {
 #pragma unroll
-                for (int q = 0; q < G; ++q) issue_one(s, q);
-        }
+                    for (int q = 0; q < A_DMA; ++q) issue_a(s, q, s * A_BYTES);
+#pragma unroll
+                    for (int q = 0; q < B_DMA; ++q) issue_b(s, q, s * B_BYTES);
+                }
+            }
+    } else {
+#pragma unroll
+        for (int s = 0; s < NSTAGE; ++s)
+            if (s < ks_count) {
+                if (s == 0 && has_tail && ks_begin == 0) issue_tail();
+                else
+#pragma unroll
+                    for (int q = 0; q < G; ++q) issue_one(s, q);
+            }
+    }
     wait_later((ks_count < NSTAGE ? ks_count : NSTAGE) - 1);
     __syncthreads();
     if constexpr (T::SCHEDULE == kByIndex) {
@@ -313,12 +334,24 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         }
         if (t < ks_count) stage(t, fr[0], fr[1]);
     } else {
+        // Stage t: behind the barrier of stage t - 1 its slabs are free.  The loads of a's stage t + NSTAGE go out over the first three
+        // sub-steps, those of b's, whose ring is one slab shorter, behind this stage's own barrier: sixteen loads in a row stood in each
+        // other's way.
         half8 fr[2][F];
+        auto fetch = [&](uint32_t slot_a, uint32_t slot_b, int sub, int f) {
+            return f < MT ? fragment_at(lds + slot_a, sub, true, wm * WTM + 32 * f) : fragment_at(lds + RING_A + slot_b, sub, false, wn * WTN + 32 * (f - MT));
+        };
 #pragma unroll
-        for (int n = 0; n < F; ++n) fr[0][order(n)] = fragment(0, 0, order(n));
-        constexpr int R = (F + NM - 1) / NM, D = (G + NM - 1) / NM;  // fragment reads and loads per matrix instruction
-        for (int t = 0; t < ks_count; ++t) {
-            const bool more = t + NSTAGE < ks_count, next = t + 1 < ks_count;
+        for (int n = 0; n < F; ++n) fr[0][order(n)] = fetch(0, 0, 0, order(n));
+        constexpr int R = (F + NM - 1) / NM;                                        // fragment reads per matrix instruction
+        constexpr int DA = (A_DMA + 3 * NM - 1) / (3 * NM), SA = 3 * NM * DA / A_DMA;  // a's loads: DA every SA-th of them
+        constexpr int DB = (B_DMA + NM - 1) / NM, SB = NM * DB / B_DMA;
+        uint32_t now_a = 0, now_b = 0;  // slots of stage t
+        auto after = [](uint32_t slot, uint32_t bytes, uint32_t ring) { return slot + bytes == ring ? 0u : slot + bytes; };
+        // (the steady state has no branch: with a test around every read and load of the last sub-step, 8192^3 took 3 % longer)
+        auto stage = [&](int t, auto more_, auto next_) {
+            constexpr bool more = decltype(more_)::value, next = decltype(next_)::value;
+            const uint32_t next_a = after(now_a, A_BYTES, RING_A), next_b = after(now_b, B_BYTES, NSTAGE * B_BYTES), last_a = after(next_a, A_BYTES, RING_A);
 #pragma unroll
             for (int sub = 0; sub < 4; ++sub) {
 #pragma unroll
@@ -329,22 +362,35 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         const int n = k * R + r;
-                        if (n < F && (sub < 3 || next)) fr[(sub + 1) & 1][order(n)] = fragment(sub < 3 ? t : t + 1, (sub + 1) & 3, order(n));
+                        if (n < F && (sub < 3 || next))
+                            fr[(sub + 1) & 1][order(n)] = fetch(sub < 3 ? now_a : next_a, sub < 3 ? now_b : next_b, (sub + 1) & 3, order(n));
                     }
-                    if (sub == 3 && more) {
+                    const int slot = sub * NM + k;
+                    if (more && sub < 3 && slot % SA == 0) {
 #pragma unroll
-                        for (int r = 0; r < D; ++r)
-                            if (k * D + r < G) issue_one(t + NSTAGE, k * D + r);
+                        for (int d = 0; d < DA; ++d)
+                            if (slot / SA * DA + d < A_DMA) issue_a(t + NSTAGE, slot / SA * DA + d, last_a);
+                    }
+                    if (more && sub == 3 && k % SB == 0) {
+#pragma unroll
+                        for (int d = 0; d < DB; ++d)
+                            if (k / SB * DB + d < B_DMA) issue_b(t + NSTAGE, k / SB * DB + d, now_b);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (sub == 2) {
-                    if (next) wait_stage(t + 1);
-                    else wait_vm_lds<63>();
+                if (sub == 2 && next) {
+                    wait_vm_lds<more ? A_DMA : 0>();
                     __syncthreads();
                 }
             }
-        }
+            now_a = next_a;
+            now_b = next_b;
+        };
+        static_assert(NSTAGE == 2, "what the waits count");
+        int t = 0;
+        for (; t + NSTAGE < ks_count; ++t) stage(t, std::true_type{}, std::true_type{});
+        for (; t + 1 < ks_count; ++t) stage(t, std::false_type{}, std::true_type{});
+        if (t < ks_count) stage(t, std::false_type{}, std::false_type{});
     }
     epi(at, acc, ahead);
 }

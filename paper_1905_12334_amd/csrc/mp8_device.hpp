@@ -371,6 +371,10 @@ struct StatsAcc {
     __device__ __forceinline__ void flush(mp8_stats *out) { flush(out, peek(out)); }
     __device__ __forceinline__ void flush(mp8_stats *out, uint32_t seen) {
         __shared__ uint32_t part[3][16];
+        flush(out, seen, part);
+    }
+    // `part`: LDS that no thread of the block uses for anything else any more.
+    __device__ __forceinline__ void flush(mp8_stats *out, uint32_t seen, uint32_t (*part)[16]) {
         uint32_t m = nan_seen ? 0x7FC00000u : f2u(amax);
         uint32_t nf = nonfinite, z = zero_codes - zero_inputs;
         reduce_wave(m, nf, z);

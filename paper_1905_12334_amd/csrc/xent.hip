@@ -100,7 +100,8 @@ struct XentStats {
             mine[i] = f32x2{base, s};
         }
         // the right-hand waves hand over to the left-hand ones
-        __shared__ f32x2 right[T::BM];
+        f32x2 *right = reinterpret_cast<f32x2 *>(at.lds);  // [BM]
+        __syncthreads();
         const int wm = at.wave / T::WGN, wn = at.wave % T::WGN;
         if (wn == 1 && at.lane < 32) {
 #pragma unroll
@@ -232,7 +233,10 @@ struct XentOut : HalfNoneAhead {
                 for (int e = 0; e < 8; ++e) xent_count_half(st, v[e]);
             }
         });
-        if (stats != nullptr) st.flush(stats, seen);
+        if (stats != nullptr) {
+            __syncthreads();  // (the bands' LDS)
+            st.flush(stats, seen, reinterpret_cast<uint32_t (*)[16]>(at.lds));
+        }
     }
 };
 
