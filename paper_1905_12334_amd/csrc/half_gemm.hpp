@@ -7,19 +7,30 @@
 
 namespace mp8 {
 
-// An operand is stored with its contraction index contiguous ([rows, kc]), or contraction-major ([kc, rows]).  Leading dimensions and
-// batch strides in bytes; addresses and both are multiples of 16.  A row-major operand is read to the next multiple of 8 of its
+// A matrix of halves: element (r, c) at r ld + (c / 64) panel + c % 64.  panel = 64: rows as usual; otherwise columns in panels of 64, which
+// matrices made here are laid out in (ld = 64, panel = 64 times the rows): what a stage needs of an operand, and what a tile stores, is
+// contiguous then but for the panels.
+struct HalfMatrix {
+    const uint16_t *p;
+    int64_t ld, panel, batch;  // in halves; batch: between matrices
+    static HalfMatrix rows(const uint16_t *p, int64_t ld) { return {p, ld, 64, 0}; }
+    static HalfMatrix panels(const uint16_t *p, int64_t rows, int64_t batch = 0) { return {p, 64, 64 * rows, batch}; }
+};
+
+// An operand is stored with its contraction index contiguous ([rows, kc]), or contraction-major ([kc, rows]).  Leading dimensions, panel and
+// batch strides in bytes; addresses and all of them are multiples of 16.  A row-major operand is read to the next multiple of 8 of its
 // contraction, where it has to hold zeros (or finite values, if the other operand holds zeros there); a contraction-major one has a
 // multiple of 8 rows.
 struct HalfGemm {
     const uint8_t *a, *b;
-    int64_t lda, ldb, a_batch, b_batch;
+    int64_t lda, ldb, a_panel, b_panel, a_batch, b_batch;
     int rows, cols;      // of the output; loads beyond them are clamped to the last row (or eight rows), and never stored
     int ksteps, tail;    // stages of 64, and the contraction indices of a last, incomplete one (0: none; see GemmArgs::tail)
     int splits, ks_per, ks_extra;
     int tiles_m, tiles_n;
     int symmetric;       // square output of which only the tiles on and above the diagonal are made
     const uint32_t *skip;  // nullable: a call that is skipped if this is not zero
+    uint32_t total;        // tiles of all slices and batches
     FastDiv div_tiles;   // by the tiles of one slice
     FastDiv div_splits;
     FastDiv div_band, div_last, div_tn;  // by 8 * tiles_n, by the height of the last band of 8 tile rows, by tiles_n
@@ -30,7 +41,7 @@ struct HalfTile {
     int batch, split, tm, tn;
 };
 
-// Consecutive workgroups go to different XCDs, each with an L2 of its own: workgroup i takes the i/8-th tile of the i%8-th eighth of
+// Consecutive workgroups go to different XCDs, each with an L2 of its own: number i is the i/8-th tile of the i%8-th eighth of
 // them, so that what runs on one XCD is a run of neighbours, in bands of eight tile rows.
 __device__ __forceinline__ HalfTile half_tile(const HalfGemm &p) {
     const uint32_t n = gridDim.x, i = blockIdx.x, q = n >> 3, r = n & 7, x = i & 7;
@@ -106,8 +117,7 @@ struct HalfPlace {
 // Gaussian operands, contraction 4096, TFLOP/s: 4096 x 4096 in 256x256 tiles 1090, in 128x128 tiles 1015 (with the other schedule 915), in
 // 64x64 tiles 570.  What bounds them: the 256x256 tile the power such data draws (all ones: 1390) and the clock it leaves
 // (1.85 GHz, 59 % of the cycles with a matrix instruction; loads that always hit, 1550), the small ones what a CU gets from L2 (14 TB/s in
-// all).  A row pitch that is a multiple of some KB costs up to 15 % (8192 x 2048 x 32768, pitch 64 KB 938, 128 bytes more 1105):
-// matrices laid out here have an odd number of 128-byte lines per row (half_pitch).
+// all).
 // Slab images:
 //   row-major: row r is 128 bytes, its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7)
 //   contraction-major: panels of 64 tile rows; 64 contraction rows of 128 bytes, chunk c of contraction row k in slot
@@ -126,40 +136,41 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
     __shared__ __attribute__((aligned(1024))) uint8_t lds[NSTAGE * STAGE + (AHEAD ? A_BYTES : 0)];
 
     if (p.skip != nullptr && *p.skip != 0u) return;
-    const HalfTile tile = half_tile(p);
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave / T::WGN, wn = wave % T::WGN;
-    const int row0 = tile.tm * BM, col0 = tile.tn * BN;
-    const int ks_begin = tile.split * p.ks_per + (tile.split < p.ks_extra ? tile.split : p.ks_extra);
-    const int ks_count = __builtin_amdgcn_readfirstlane(p.ks_per + (tile.split < p.ks_extra ? 1 : 0));
 
     const bool has_tail = p.tail != 0;
-    const int first = ks_begin - (has_tail ? 1 : 0);  // stage s of this slice covers indices 64 (first + s) ..
-    const int64_t a_kstep = ATN ? 64 * p.lda : 128, b_kstep = BTN ? 64 * p.ldb : 128;
-    const uint8_t *a_tile = uniform_ptr(p.a + tile.batch * p.a_batch + (ATN ? 2 * (int64_t)row0 : row0 * p.lda) + first * a_kstep);
-    const uint8_t *b_tile = uniform_ptr(p.b + tile.batch * p.b_batch + (BTN ? 2 * (int64_t)col0 : col0 * p.ldb) + first * b_kstep);
+    const int64_t a_kstep = ATN ? 64 * p.lda : p.a_panel, b_kstep = BTN ? 64 * p.ldb : p.b_panel;
 
     // load q of this wave: the slab's KB u = wave + 4 q
     auto krow = [&](int q) { return 8 * ((wave + 4 * q) & 7) + (lane >> 3); };  // contraction-major: of the stage's 64
     const int lchunk = (lane & 7) ^ ((4 * wave + (lane >> 4)) & 7), lchunk_t = (lane & 7) ^ (((lane >> 4) & 1) << 2);
-    auto offset = [&](bool km, int q, int origin, int extent, int64_t ld) -> uint32_t {
+    auto offset = [&](bool km, int q, int origin, int extent, int64_t ld, int64_t panel) -> uint32_t {
         if (km) {
             int m = 64 * ((wave + 4 * q) >> 3) + 8 * lchunk_t;
             m = origin + m + 8 <= extent ? m : extent - 8 - origin;
-            return (uint32_t)(krow(q) * ld + 2 * m);
+            return (uint32_t)(krow(q) * ld + (m >> 6) * panel + 2 * (m & 63));
         }
         int r = 8 * (wave + 4 * q) + (lane >> 3);
         r = origin + r < extent ? r : extent - 1 - origin;
         return (uint32_t)(r * ld) + 16 * lchunk;
     };
-    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane, lds};
-    auto ahead = epi.ahead(at);  // what the epilogue wants to have read by then
+    const HalfTile tile = half_tile(p);
+    const int row0 = tile.tm * BM, col0 = tile.tn * BN;
+    const int ks_begin = tile.split * p.ks_per + (tile.split < p.ks_extra ? tile.split : p.ks_extra);
+    const int ks_count = __builtin_amdgcn_readfirstlane(p.ks_per + (tile.split < p.ks_extra ? 1 : 0));
+    const int first = ks_begin - (has_tail ? 1 : 0);  // stage s of this slice covers indices 64 (first + s) ..
+    const bool tail_first = has_tail && ks_begin == 0;
+    const uint8_t *a_tile = uniform_ptr(p.a + tile.batch * p.a_batch + (ATN ? (row0 >> 6) * p.a_panel : row0 * p.lda) + first * a_kstep);
+    const uint8_t *b_tile = uniform_ptr(p.b + tile.batch * p.b_batch + (BTN ? (col0 >> 6) * p.b_panel : col0 * p.ldb) + first * b_kstep);
     uint32_t oa[A_DMA], ob[B_DMA];
 #pragma unroll
-    for (int q = 0; q < A_DMA; ++q) oa[q] = offset(ATN, q, row0, p.rows, p.lda);
+    for (int q = 0; q < A_DMA; ++q) oa[q] = offset(ATN, q, row0, p.rows, p.lda, p.a_panel);
 #pragma unroll
-    for (int q = 0; q < B_DMA; ++q) ob[q] = offset(BTN, q, col0, p.cols, p.ldb);
+    for (int q = 0; q < B_DMA; ++q) ob[q] = offset(BTN, q, col0, p.cols, p.ldb, p.b_panel);
+    const HalfPlace<T> at{tile.batch, tile.split, tile.tm, tile.tn, row0 + wm * WTM, col0 + wn * WTN, wave, lane, lds};
+    auto ahead = epi.ahead(at);  // what the epilogue wants to have read by then
     const uint32_t lds0 = lds_address(lds);
     auto issue_one = [&](int s, int q) {  // load q (0 .. G-1) of stage s
         const uint32_t at = lds0 + (s % NSTAGE) * STAGE + wave * 1024;
@@ -225,7 +236,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
         for (int s = 0; s < NSTAGE; ++s)
             if (s < ks_count) {
-                if (s == 0 && has_tail && ks_begin == 0) issue_tail();
+                if (s == 0 && tail_first) issue_tail();
                 else {
 #pragma unroll
                     for (int q = 0; q < A_DMA; ++q) issue_a(s, q, s * A_BYTES);
@@ -237,7 +248,7 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
 #pragma unroll
         for (int s = 0; s < NSTAGE; ++s)
             if (s < ks_count) {
-                if (s == 0 && has_tail && ks_begin == 0) issue_tail();
+                if (s == 0 && tail_first) issue_tail();
                 else
 #pragma unroll
                     for (int q = 0; q < G; ++q) issue_one(s, q);
@@ -403,14 +414,34 @@ __device__ __forceinline__ u32x4 half_operand8(const float v[8]) {
     return __builtin_bit_cast(u32x4, h);
 }
 
-// Sixteen columns of accumulator elements 4 g .. 4 g + 7 (g even), packed as such halves: the lower half wave ends up with columns
-// 8 g .. +7 of the 32, the upper one with the eight after them, sixteen bytes each.
-__device__ __forceinline__ u32x4 half_pack16(const float v[8]) {
-    const u32x4 w = half_operand8(v);
-    const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
-    const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-    return u32x4{s0[0], s1[0], s0[1], s1[1]};
-}
+// Rows of halves through LDS, so that a store covers whole 128-byte lines (pieces of 32 bytes, as the accumulators lie, kept the L2 busy
+// for as long as four times their size: 8192 x 32768 halves in 256x256 tiles 9 us per round of tiles).  A band of 32 rows of a wave's
+// part takes WTN * 64 bytes; 16-byte chunk c of row r sits in slot c ^ (r & mask), and its halves change places in rows 16 .. 31, which
+// keeps the lanes of a write apart.  LDS operations of a wave are done in order.
+template <class T>
+struct HalfLines {
+    static constexpr int PER = T::WTN / 8, MASK = (PER & (PER - 1)) == 0 ? PER - 1 : 3, ROWS = 64 / PER, PASSES = (32 + ROWS - 1) / ROWS;
+    uint8_t *band;
+    int lane;
+    __device__ __forceinline__ HalfLines(const HalfPlace<T> &at) : band(at.lds + at.wave * T::WTN * 64), lane(at.lane) {}
+    // four columns from 32 j + 8 g + 4 (lane / 32) on of row lane % 32
+    __device__ __forceinline__ void put(int j, int g, u32x2 v) {
+        const int r = lane & 31, h = lane >> 5;
+        *reinterpret_cast<u32x2 *>(band + r * T::WTN * 2 + (((4 * j + g) ^ (r & MASK)) << 4) + 8 * (h ^ (r >> 4))) = v;
+    }
+    // f(row, first of eight columns, halves) for the band's rows
+    template <class F>
+    __device__ __forceinline__ void each(const F &f) {
+        const int lr = lane / PER, c = lane % PER;
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            const int r = ROWS * k + lr;
+            if (64 % PER != 0 && (lr >= ROWS || r >= 32)) continue;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(band + r * T::WTN * 2 + ((c ^ (r & MASK)) << 4));
+            f(r, 8 * c, r < 16 ? v : u32x4{v.z, v.w, v.x, v.y});
+        }
+    }
+};
 
 // f(r, c, v, x) for every eight neighbouring columns c .. c+7 of rows r of the wave's part, x = load(r, c): bands of 32 rows pass through
 // LDS (a region of the ring per wave), so that the lanes that share a row lie side by side and store and load whole 128-byte lines, and
@@ -551,15 +582,17 @@ static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int6
 }
 
 // The geometry of a call.  Sizes have been checked: rows, cols, kc >= 1 and what HalfGemm says.
-static inline HalfGemm half_gemm_args(const void *a, int64_t lda, int64_t a_batch, const void *b, int64_t ldb, int64_t b_batch, int64_t rows,
-                                      int64_t cols, int64_t kc, int tile_m, int tile_n, int splits, bool symmetric) {
+static inline HalfGemm half_gemm_args(const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t cols, int64_t kc, int tile, int splits,
+                                      bool symmetric, int64_t batch) {
     HalfGemm p{};
-    p.a = (const uint8_t *)a;
-    p.b = (const uint8_t *)b;
-    p.lda = 2 * lda;
-    p.ldb = 2 * ldb;
-    p.a_batch = 2 * a_batch;
-    p.b_batch = 2 * b_batch;
+    p.a = (const uint8_t *)a.p;
+    p.b = (const uint8_t *)b.p;
+    p.lda = 2 * a.ld;
+    p.ldb = 2 * b.ld;
+    p.a_panel = 2 * a.panel;
+    p.b_panel = 2 * b.panel;
+    p.a_batch = 2 * a.batch;
+    p.b_batch = 2 * b.batch;
     p.rows = (int)rows;
     p.cols = (int)cols;
     p.ksteps = (int)((kc + 63) / 64);
@@ -567,10 +600,11 @@ static inline HalfGemm half_gemm_args(const void *a, int64_t lda, int64_t a_batc
     p.splits = splits;
     p.ks_per = p.ksteps / splits;
     p.ks_extra = p.ksteps % splits;
-    p.tiles_m = (int)((rows + tile_m - 1) / tile_m);
-    p.tiles_n = (int)((cols + tile_n - 1) / tile_n);
+    p.tiles_m = (int)((rows + tile - 1) / tile);
+    p.tiles_n = (int)((cols + tile - 1) / tile);
     p.symmetric = symmetric;
     const int tiles = symmetric ? p.tiles_m * (p.tiles_m + 1) / 2 : p.tiles_m * p.tiles_n;
+    p.total = (uint32_t)((int64_t)tiles * splits * batch);
     p.div_tiles = make_fastdiv((uint32_t)tiles);
     p.div_splits = make_fastdiv((uint32_t)splits);
     p.div_band = make_fastdiv((uint32_t)(8 * p.tiles_n));
@@ -580,21 +614,19 @@ static inline HalfGemm half_gemm_args(const void *a, int64_t lda, int64_t a_batc
 }
 
 template <class T, bool ATN, bool BTN, class Epi>
-static inline bool half_gemm_launch(const HalfGemm &p, int64_t batch, const Epi &epi, hipStream_t stream) {
-    const int64_t tiles = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
-    hipLaunchKernelGGL((half_gemm_kernel<T, ATN, BTN, Epi>), dim3((unsigned)(tiles * p.splits * batch)), dim3(256), 0, stream, p, epi);
+static inline bool half_gemm_launch(const HalfGemm &p, const Epi &epi, hipStream_t stream) {
+    hipLaunchKernelGGL((half_gemm_kernel<T, ATN, BTN, Epi>), dim3(p.total), dim3(256), 0, stream, p, epi);
     return hipGetLastError() == hipSuccess;
 }
 
 // The tiles of a plan.
 template <bool ATN, bool BTN, class Epi>
-static inline bool half_gemm_launch_plan(int tile, const HalfGemm &p, int64_t batch, const Epi &epi, hipStream_t stream) {
-    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, batch, epi, stream);
-    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, batch, epi, stream);
-    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, batch, epi, stream);
-    const int64_t tiles = p.symmetric ? (int64_t)p.tiles_m * (p.tiles_m + 1) / 2 : (int64_t)p.tiles_m * p.tiles_n;
-    if (half_by_index(tiles * p.splits * batch, (double)p.ks_per)) return half_gemm_launch<Half64Few, ATN, BTN>(p, batch, epi, stream);
-    return half_gemm_launch<Half64, ATN, BTN>(p, batch, epi, stream);
+static inline bool half_gemm_launch_plan(int tile, const HalfGemm &p, const Epi &epi, hipStream_t stream) {
+    if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, epi, stream);
+    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, epi, stream);
+    if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, epi, stream);
+    if (half_by_index(p.total, (double)p.ks_per)) return half_gemm_launch<Half64Few, ATN, BTN>(p, epi, stream);
+    return half_gemm_launch<Half64, ATN, BTN>(p, epi, stream);
 }
 
 }  // namespace mp8

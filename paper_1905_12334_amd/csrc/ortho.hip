@@ -363,17 +363,13 @@ mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
     return MP8_OK;
 }
 
-struct OrthoOperand {
-    const uint16_t *p;
-    int64_t ld, batch;
-};
 template <bool ATN, bool BTN, class Epi>
-bool ortho_product(int64_t batch, const OrthoOperand &a, const OrthoOperand &b, int64_t rows, int64_t cols, int64_t kc, bool symmetric,
+bool ortho_product(int64_t batch, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t cols, int64_t kc, bool symmetric,
                    const uint32_t *skip, const Epi &epi, hipStream_t stream) {
     const int tile = half_plan(batch, rows, cols, kc, symmetric, 1).tile;
-    HalfGemm p = half_gemm_args(a.p, a.ld, a.batch, b.p, b.ld, b.batch, rows, cols, kc, tile, tile, 1, symmetric);
+    HalfGemm p = half_gemm_args(a, b, rows, cols, kc, tile, 1, symmetric, batch);
     p.skip = skip;
-    return half_gemm_launch_plan<ATN, BTN>(tile, p, batch, epi, stream);
+    return half_gemm_launch_plan<ATN, BTN>(tile, p, epi, stream);
 }
 
 }  // namespace
@@ -418,9 +414,9 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const int64_t blocks = up(rows * (c8 / 8), 256) / 256;
     hipLaunchKernelGGL(ortho_start_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)batch), dim3(256), 0, st, start);
     if (!ok()) return MP8_ERR_HIP;
-    const OrthoOperand A{a, l.lda, ab}, P{b, l.lda, ab};
+    const HalfMatrix A{a, l.lda, 64, ab}, P{b, l.lda, 64, ab};
     for (int k = 0; k < steps; ++k) {
-        const OrthoOperand X{x[k & 1], l.ld, xb};
+        const HalfMatrix X{x[k & 1], l.ld, 64, xb};
         const OrthoSymmetric<false> gram{{}, nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
         if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
                          : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))

@@ -61,26 +61,27 @@ struct XentStats {
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Ahead<T::MT> &a) const {
         const int h4 = 4 * (at.lane >> 5), left = N - at.col0;  // columns of this wave's tile that exist
         f32x2 mine[T::MT];
+        // The (base, sum) of a row's accumulators.  Most waves have neither a target among their columns nor columns that do not exist;
+        // with both tests in one path for all, 4096 x 32000 x 512 took 268 us in 256x256 tiles.
+        auto row_sum = [&](int i, auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            f32x16 z[T::NT];
 #pragma unroll
-        for (int i = 0; i < T::MT; ++i) {
-            f32x16 (&z)[T::NT] = acc[i];
-            if (left < T::WTN) {
+            for (int j = 0; j < T::NT; ++j) z[j] = acc[i][j];
+            if constexpr (!PLAIN) {
+                int end = left - h4, c = a.target[i] - h4;  // (-1 - 4 h meets no column)
+                asm volatile("" : "+v"(end), "+v"(c));  // (the comparisons anew in every row: sixty-four masks do not fit the registers)
+                float zt = 0.0f;
 #pragma unroll
                 for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (32 * j + 8 * (e >> 2) + h4 + (e & 3) >= left) z[j][e] = -__builtin_inff();
-            }
-            if (__builtin_amdgcn_ballot_w64(a.target[i] >= 0) != 0) {
-                const int c = a.target[i] - h4;  // (-1 - 4 h meets no column)
-#pragma unroll
-                for (int j = 0; j < T::NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (c == 32 * j + 8 * (e >> 2) + (e & 3)) {
-                            z_target[at.row(i)] = z[j][e];
-                            z[j][e] = -__builtin_inff();
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        const int column = 32 * j + 8 * (e >> 2) + (e & 3);
+                        zt = c == column ? z[j][e] : zt;
+                        z[j][e] = c == column || column >= end ? -__builtin_inff() : z[j][e];
+                    }
+                // (of the two lanes of the row the one that holds the column)
+                if (a.target[i] >= 0 && ((a.target[i] >> 2) & 1) == (at.lane >> 5)) z_target[at.row(i)] = zt;
             }
             float m = -__builtin_inff();
 #pragma unroll
@@ -90,14 +91,20 @@ struct XentStats {
             const auto both = __builtin_amdgcn_permlane32_swap(f2u(m), f2u(m), false, false);
             m = __builtin_fmaxf(u2f(both[0]), u2f(both[1]));
             const float base = m == -__builtin_inff() ? 0.0f : m * kLog2e;
-            float s = 0.0f;
+            float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};  // (four chains of additions)
 #pragma unroll
             for (int j = 0; j < T::NT; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base));
-            const auto sums = __builtin_amdgcn_permlane32_swap(f2u(s), f2u(s), false, false);
-            s = u2f(sums[0]) + u2f(sums[1]);
-            mine[i] = f32x2{base, s};
+                for (int e = 0; e < 16; ++e) s[e & 3] += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], kLog2e, -base));
+            const float four = (s[0] + s[1]) + (s[2] + s[3]);
+            const auto sums = __builtin_amdgcn_permlane32_swap(f2u(four), f2u(four), false, false);
+            mine[i] = f32x2{base, u2f(sums[0]) + u2f(sums[1])};
+        };
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            __builtin_amdgcn_sched_barrier(0);  // (one row of accumulators at a time: together they overflow the registers)
+            if (left >= T::WTN && __builtin_amdgcn_ballot_w64(a.target[i] >= 0) == 0) row_sum(i, std::true_type{});
+            else row_sum(i, std::false_type{});
         }
         // the right-hand waves hand over to the left-hand ones
         f32x2 *right = reinterpret_cast<f32x2 *>(at.lds);  // [BM]
@@ -119,11 +126,13 @@ struct XentStats {
 };
 
 // e of a tile, as halves times 2^14 and the token's weight.
+using half4 = _Float16 __attribute__((ext_vector_type(4)));
 struct XentError {
     const int64_t *targets;
     const float *loss, *lse, *factor;  // factor [M]: 2^14 and the token's weight; 0 without a target
-    uint16_t *out;                     // [M, ld]
-    int64_t ld;
+    uint16_t *out;                     // panels of 64 columns, `wide` columns in all
+    int64_t panel;
+    int wide;
     int M, N, first;                   // N: columns that exist; those behind them, to the tile's end, become zero
     template <int MT>
     struct Ahead {
@@ -147,39 +156,51 @@ struct XentError {
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Ahead<T::MT> &a) const {
         const int h4 = 4 * (at.lane >> 5), left = N - at.col0;
+        HalfLines<T> lines(at);
+        __syncthreads();  // (LDS: the last stage's fragments have been read everywhere)
+        auto row_errors = [&](int i, auto plain) {
+            constexpr bool PLAIN = decltype(plain)::value;
+            const float f = a.factor[i];
+            // |f| 2^(z log2 e - lse log2 e) with one exponent; a masked token's (its logits are 0, its lse may be anything) is minus infinity
+            const float shift = f == 0.0f ? -__builtin_inff() : __builtin_amdgcn_logf(__builtin_fabsf(f)) - a.base[i] * kLog2e;
+            const uint32_t sign = f < 0.0f ? 0x80008000u : 0u;
+            // exp(-loss) - 1: the target's probability is one less what the others have, to the loss's precision
+            float at_target = 0.0f;
+            int end = 0, c = -1;
+            if constexpr (!PLAIN) {
+                at_target = __builtin_fabsf(f) * expm1f(-a.at_target[i]);
+                end = left - h4;
+                c = a.target[i] - h4;  // (-1 - 4 h meets no column)
+                asm volatile("" : "+v"(end), "+v"(c));  // (the comparisons anew in every row: they would all be kept)
+            }
+#pragma unroll
+            for (int j = 0; j < T::NT; ++j)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    half4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int column = 32 * j + 8 * g + e;
+                        float y = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * g + e], kLog2e, shift));
+                        if constexpr (!PLAIN) y = c == column ? at_target : column >= end ? 0.0f : y;
+                        v[e] = (_Float16)y;
+                    }
+                    u32x2 w = __builtin_bit_cast(u32x2, v);
+                    w.x ^= sign;
+                    w.y ^= sign;
+                    lines.put(j, g, w);
+                }
+        };
 #pragma unroll
         for (int i = 0; i < T::MT; ++i) {
-            const int r = at.row(i);
-            const bool row = r < M;
-            const float f = a.factor[i], base = a.base[i] * kLog2e;
-            const bool any = __builtin_amdgcn_ballot_w64(a.target[i] >= 0) != 0;
-            const int c = a.target[i] - h4;  // (-1 - 4 h meets no column)
-            // exp(-loss) - 1: the target's probability is one less what the others have, to the loss's precision
-            const float e_target = any ? f * expm1f(-a.at_target[i]) : 0.0f;
-#pragma unroll
-            for (int j = 0; j < T::NT; ++j) {
-                if (at.col0 + 32 * j >= ld) break;
-#pragma unroll
-                for (int g = 0; g < 4; g += 2) {
-                    float v[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = f * __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * g + e], kLog2e, -base));
-                    if (any) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (c == 32 * j + 8 * g + 8 * (e >> 2) + (e & 3)) v[e] = e_target;
-                    }
-                    if (left < T::WTN) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            if (32 * j + 8 * g + 8 * (e >> 2) + h4 + (e & 3) >= left) v[e] = 0.0f;
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = f == 0.0f ? 0.0f : v[e];  // (a masked token's lse may be anything)
-                    const u32x4 o = half_pack16(v);
-                    if (row) *reinterpret_cast<u32x4 *>(out + r * ld + at.col0 + 32 * j + 8 * g + 8 * (at.lane >> 5)) = o;
-                }
-            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (left >= T::WTN && __builtin_amdgcn_ballot_w64(a.target[i] >= 0) == 0) row_errors(i, std::true_type{});
+            else row_errors(i, std::false_type{});
+            lines.each([&](int r, int c, const u32x4 &v) {
+                const int row = at.row0 + 32 * i + r;
+                // (read again when it has left the caches: 8192 x 32768 x 2048 984 -> 958 us, in 128x128 tiles 1240 -> 1109)
+                if (row < M && at.col0 + c < wide) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + ((at.col0 + c) >> 6) * panel + 64 * row + ((at.col0 + c) & 63)));
+            });
         }
     }
 };
@@ -453,16 +474,15 @@ struct Layout {
     size_t factor, exponent, e, dx, dw, total;  // backward: (copies as above,) the tokens' factors, e, FP32 sums
 };
 // The logits' tiles: their epilogues take longer than others, and two workgroups per CU hide them behind each other's products.  Measured,
-// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 215 / 174, 1021 x 32003 x 1000 90 / 78, 6007 x 37003 x 1000 598 / 630,
-// 8192 x 131072 x 2048 4060 / 4540.
+// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 160 / 155, 8192 x 32768 x 2048 905 / 1032; the errors 184 / 183, 958 / 1109.
 HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
     HalfPlan best = half_plan(1, M, cols, K, false, 1);
     if (best.tile == 64) return best;
     double least = 1e300;
     for (const int tile : {256, 128}) {
-        const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 12.0 : 4.5;
+        const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 8.0 : 4.0;
         const double rounds = std::ceil((double)(((M + tile - 1) / tile) * ((cols + tile - 1) / tile)) / slots);
-        const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.73 : 1.03) + (rounds + 1.0) * epilogue;
+        const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.6 : 0.97) + (rounds + 1.0) * epilogue;
         if (t < least) {
             least = t;
             best.tile = tile;
@@ -509,7 +529,7 @@ Layout make_layout(const Shape &s, bool backward, bool dx, bool dw) {
     } else {
         l.factor = take(4 * s.M);
         l.exponent = take(4);
-        l.e = take(2 * s.M * half_pitch(s.piece));
+        l.e = take(2 * s.M * up(s.piece, 64));
         const BwdPlans p = bwd_plans(s);
         if (dx && !p.dx_direct) l.dx = take(4 * p.dx.splits * s.M * s.Kp);
         if (dw && !p.dw_direct) l.dw = take(4 * p.dw.splits * s.piece * s.Kp);
@@ -530,10 +550,8 @@ mp8_status check_sizes(int64_t M, int64_t N, int64_t K, int64_t ldx, int64_t ldw
 }
 
 template <bool BTN, bool ATN, class Epi>
-bool product(int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t cols, int64_t kc, int splits,
-             const Epi &epi, hipStream_t stream) {
-    const HalfGemm p = half_gemm_args(a, lda, 0, b, ldb, 0, rows, cols, kc, tile, tile, splits, false);
-    return half_gemm_launch_plan<ATN, BTN>(tile, p, 1, epi, stream);
+bool product(int tile, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t cols, int64_t kc, int splits, const Epi &epi, hipStream_t stream) {
+    return half_gemm_launch_plan<ATN, BTN>(tile, half_gemm_args(a, b, rows, cols, kc, tile, splits, false, 1), epi, stream);
 }
 
 bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t ld, int64_t rows, int64_t cols,
@@ -596,7 +614,7 @@ extern "C" mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K,
         }
         const int tile = logits_plan(M, cols, K).tile;
         const XentStats epi{targets, (f32x2 *)(ws + l.part), (float *)(ws + l.z_target), (int)M, (int)cols, (int)c, parts};
-        if (!product<false, false>(tile, xs, ld_x, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        if (!product<false, false>(tile, HalfMatrix::rows(xs, ld_x), HalfMatrix::rows(wp, ld_w), M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
         parts += (int)((cols + tile - 1) / tile);
     }
     const int per = M >= 512 ? 8 : 1;
@@ -635,7 +653,8 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
         hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, dloss, factor, exponent, (int)M, (int)N);
         if (hipGetLastError() != hipSuccess) return MP8_ERR_HIP;
     }
-    const int64_t K8 = up(K, 8), lde = half_pitch(s.piece);
+    const int64_t K8 = up(K, 8);
+    const HalfMatrix E = HalfMatrix::panels(e, M), X = HalfMatrix::rows(xs, s.Kp);
     const BwdPlans plans = bwd_plans(s);
     auto finish = [&](const float *sum, int64_t slab, int slabs, int64_t rows, int64_t row0, uint16_t *out16, uint8_t *out8, uint64_t offset,
                       mp8_stats *stats) {
@@ -649,11 +668,11 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
         return hipGetLastError() == hipSuccess;
     };
     // (a, b) -> rows [row0, row0 + rows) of a gradient, complete
-    auto direct = [&](auto atn, int tile, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
+    auto direct = [&](auto atn, int tile, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
                       uint8_t *out8, uint64_t offset, mp8_stats *stats) {
         constexpr bool ATN = decltype(atn)::value;
         const XentOut epi{{}, exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0, seed, offset, stats};
-        return product<true, ATN>(tile, a, lda, b, ldb, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
+        return product<true, ATN>(tile, a, b, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
     };
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
@@ -664,22 +683,23 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
             wp = (uint16_t *)(ws + l.w);
             ld_w = s.Kp;
         }
-        const XentError epi{targets, loss, lse, factor, e, lde, (int)M, (int)cols, (int)c};
-        if (!product<false, false>(logits_plan(M, cols, K).tile, xs, s.Kp, wp, ld_w, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        const HalfMatrix W = HalfMatrix::rows(wp, ld_w);
+        const XentError epi{targets, loss, lse, factor, e, E.panel, (int)up(cols, 64), (int)M, (int)cols, (int)c};
+        if (!product<false, false>(logits_plan(M, cols, K).tile, X, W, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
         if (dx) {
             if (plans.dx_direct) {
-                if (!direct(std::false_type{}, plans.dx.tile, e, lde, wp, ld_w, M, cols, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
+                if (!direct(std::false_type{}, plans.dx.tile, E, W, M, cols, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
             } else {
                 const HalfEpiSum sum{{}, dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
-                if (!product<true, false>(plans.dx.tile, e, lde, wp, ld_w, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
+                if (!product<true, false>(plans.dx.tile, E, W, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
             }
         }
         if (dw) {
             if (plans.dw_direct) {
-                if (!direct(std::true_type{}, plans.dw.tile, e, lde, xs, s.Kp, cols, M, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
+                if (!direct(std::true_type{}, plans.dw.tile, E, X, cols, M, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             } else {
                 const HalfEpiSum sum{{}, dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
-                if (!product<true, true>(plans.dw.tile, e, lde, xs, s.Kp, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
+                if (!product<true, true>(plans.dw.tile, E, X, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
                 if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             }
         }
