@@ -13,6 +13,7 @@ namespace mp8 {
 struct HalfMatrix {
     const uint16_t *p;
     int64_t ld, panel, batch;  // in halves; batch: between matrices
+    static __host__ __device__ int64_t at(int64_t r, int64_t c, int64_t panel) { return (c >> 6) * panel + 64 * r + (c & 63); }  // in panels
     static HalfMatrix rows(const uint16_t *p, int64_t ld) { return {p, ld, 64, 0}; }
     static HalfMatrix panels(const uint16_t *p, int64_t rows, int64_t batch = 0) { return {p, 64, 64 * rows, batch}; }
 };
@@ -538,9 +539,6 @@ struct HalfEpiSum : HalfNoneAhead {
 // ---------------------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------------------
-// Row pitch in halves of a matrix that is laid out here: whole 128-byte lines, an odd number of them.
-static inline int64_t half_pitch(int64_t n) { return ((n + 63) / 64 | 1) * 64; }
-
 // Which tiles a product takes and into how many slices its contraction is cut.
 struct HalfPlan {
     int tile, splits;

@@ -7,7 +7,7 @@
 // A step maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors alone: with (a, b, c) = (3.4445,
 // -4.7750, 2.0315), whose slope at zero is steep, five steps bring all but the smallest to 0.7 .. 1.2.
 //
-// X lies as the weights do, [rows, ld].  A is formed over the shorter side: X X^T and (bA + cA^2) X where rows <= cols, X^T X and
+// X has the weights' rows and columns, in panels of 64 columns, and so have A and the polynomial.  A is formed over the shorter side: X X^T and (bA + cA^2) X where rows <= cols, X^T X and
 // X (bA + cA^2) otherwise; the second product of the last step updates the weights itself.  Operands of the products are
 // halves, sums FP32.  A power of two keeps each of them in the format's range: singular values stay below 1.21, so that entries of A
 // are below 1.46 and those of bA + cA^2 below 2.81 in magnitude; A and the polynomial are stored times 2^14, X times S = 2^round(log2
@@ -39,7 +39,7 @@ template <bool POLY>
 struct OrthoSymmetric : HalfNoneAhead {
     const uint16_t *in;
     uint16_t *out;
-    int64_t ld, batch;   // in halves
+    int64_t panel, batch;  // in halves
     int m;
     float linear, scale;
     template <class T>
@@ -49,7 +49,7 @@ struct OrthoSymmetric : HalfNoneAhead {
         const bool mirror = at.tm != at.tn;
         auto load = [&](int r, int c) {
             u32x4 xw = {0, 0, 0, 0};
-            if (POLY && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + r * ld + c);
+            if (POLY && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + HalfMatrix::at(r, c, panel));
             return xw;
         };
         auto value = [&](const u32x4 &xw, const float (&sum)[8]) {
@@ -67,7 +67,7 @@ struct OrthoSymmetric : HalfNoneAhead {
                 for (int e = 0; e < 8; ++e)
                     if (e >= m - c) w[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
             }
-            *reinterpret_cast<u32x4 *>(o + r * ld + c) = w;
+            *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(r, c, panel)) = w;
         }, [&](int i, const float *band) {
             if (!mirror) return;
             // four lanes per row of the turned band: its rows are the band's columns, its columns rows of the tile, all of which exist
@@ -85,7 +85,7 @@ struct OrthoSymmetric : HalfNoneAhead {
                     float sum[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
-                    if (c < m) *reinterpret_cast<u32x4 *>(o + c * ld + r) = value(xw[u], sum);
+                    if (c < m) *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(c, r, panel)) = value(xw[u], sum);
                 }
             }
         });
@@ -96,18 +96,18 @@ struct OrthoSymmetric : HalfNoneAhead {
 struct OrthoNext : HalfNoneAhead {
     const uint16_t *x;
     uint16_t *out;
-    int64_t ld, batch; // in halves
+    int64_t panel, batch;  // in halves
     int rows, cols;
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
         const int64_t base = at.batch * batch;
         half_bands(at, acc, [&](int r, int c) {
             u32x4 xw = {0, 0, 0, 0};
-            if (r < rows && c < cols) xw = *reinterpret_cast<const u32x4 *>(x + base + r * ld + c);
+            if (r < rows && c < cols) xw = *reinterpret_cast<const u32x4 *>(x + base + HalfMatrix::at(r, c, panel));
             return xw;
         }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
             if (r >= rows || c >= cols) return;
-            *reinterpret_cast<u32x4 *>(out + base + r * ld + c) = ortho_combine(kOrthoA, xw, kDown, sum);
+            *reinterpret_cast<u32x4 *>(out + base + HalfMatrix::at(r, c, panel)) = ortho_combine(kOrthoA, xw, kDown, sum);
         }, [](int, float *) {});
     }
 };
@@ -115,7 +115,7 @@ struct OrthoNext : HalfNoneAhead {
 // The last iterate goes straight into the weights: w' = w - lr (X + wd w), rounded to half, and its 8-bit copy.
 struct OrthoUpdate : HalfNoneAhead {
     const uint16_t *x;
-    int64_t ld, batch;
+    int64_t panel, batch;
     int rows, cols;
     float inv_s, neg_lr, wd;
     uint16_t *w16;
@@ -134,7 +134,7 @@ struct OrthoUpdate : HalfNoneAhead {
         half_bands<(T::BM > 128 ? 1 : 4)>(at, acc, [&](int r, int c) {
             Eight in{};
             if (r >= rows || c >= cols) return in;
-            in.x = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + r * ld + c);
+            in.x = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + HalfMatrix::at(r, c, panel));
             const int64_t i0 = first + (int64_t)r * cols + c;
             if (whole) {
                 in.w = *reinterpret_cast<const u32x4 *>(w16 + i0);
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(256) void ortho_momentum_kernel(const OrthoMomentum
     }
 }
 
-// X0 times S as halves, [rows, ld] per matrix, from the new momentum and the gradient: eight columns per thread, zeros behind the last.
+// X0 times S as halves, in panels, from the new momentum and the gradient: eight columns per thread, zeros behind the last.
 struct OrthoStart {
     const float *v;
     const uint8_t *g8;
@@ -267,7 +267,7 @@ struct OrthoStart {
     const uint32_t *skip;
     double s;
     uint16_t *x;
-    int64_t ld, batch;
+    int64_t batch;
     FastDiv div_groups;  // by the groups of eight in a row, cols / 8 rounded up
 };
 __global__ __launch_bounds__(256) void ortho_start_kernel(const OrthoStart p) {
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const OrthoStart p) {
             }
             o[q] = h[0] | (h[1] << 16);
         }
-        *reinterpret_cast<u32x4 *>(p.x + blockIdx.y * p.batch + r * p.ld + c) = o;
+        *reinterpret_cast<u32x4 *>(p.x + blockIdx.y * p.batch + HalfMatrix::at(r, c, 64 * (int64_t)p.rows)) = o;
     }
 }
 
@@ -326,7 +326,7 @@ namespace {
 int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct OrthoLayout {
-    int64_t m, n, ld, lda;  // shorter and longer side; X [rows, ld], A [m, lda]
+    int64_t m, n, x_batch, a_batch;  // shorter and longer side; halves of an X and of an A
     int blocks;             // workgroups of the momentum pass per matrix
     size_t squares, x0, x1, a, b, total;
 };
@@ -334,8 +334,8 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     OrthoLayout l{};
     l.m = rows < cols ? rows : cols;
     l.n = rows < cols ? cols : rows;
-    l.ld = half_pitch(cols);
-    l.lda = half_pitch(l.m);
+    l.x_batch = rows * up(cols, 64);
+    l.a_batch = l.m * up(l.m, 64);
     const int64_t want = (rows * cols + 4095) / 4096, most = batch >= 256 ? 4 : 1024 / batch;
     l.blocks = (int)(want < 1 ? 1 : want > most ? most : want);
     size_t at = 0;
@@ -345,10 +345,10 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
         return here;
     };
     l.squares = take(8 * batch * l.blocks);
-    l.x0 = take(2 * batch * rows * l.ld);
-    l.x1 = take(2 * batch * rows * l.ld);
-    l.a = take(2 * batch * l.m * l.lda);
-    l.b = take(2 * batch * l.m * l.lda);
+    l.x0 = take(2 * batch * l.x_batch);
+    l.x1 = take(2 * batch * l.x_batch);
+    l.a = take(2 * batch * l.a_batch);
+    l.b = take(2 * batch * l.a_batch);
     l.total = at;
     return l;
 }
@@ -408,28 +408,28 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const OrthoMomentum mom{velocity, g8, rows * cols, inv_loss_scale, momentum, nesterov, l.blocks, skip_if_nonzero, squares, stats};
     hipLaunchKernelGGL(ortho_momentum_kernel, dim3((unsigned)l.blocks, (unsigned)batch), dim3(256), 0, st, mom);
     if (!ok()) return MP8_ERR_HIP;
-    const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = rows * l.ld, ab = l.m * l.lda;
-    const OrthoStart start{velocity, g8, (int)rows, (int)cols, inv_loss_scale, momentum, nesterov, l.blocks, squares, skip_if_nonzero, s, x[0], l.ld, xb,
+    const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = l.x_batch, ab = l.a_batch, x_panel = 64 * rows, a_panel = 64 * l.m;
+    const OrthoStart start{velocity, g8, (int)rows, (int)cols, inv_loss_scale, momentum, nesterov, l.blocks, squares, skip_if_nonzero, s, x[0], xb,
                            make_fastdiv((uint32_t)(c8 / 8))};
     const int64_t blocks = up(rows * (c8 / 8), 256) / 256;
     hipLaunchKernelGGL(ortho_start_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)batch), dim3(256), 0, st, start);
     if (!ok()) return MP8_ERR_HIP;
-    const HalfMatrix A{a, l.lda, 64, ab}, P{b, l.lda, 64, ab};
+    const HalfMatrix A = HalfMatrix::panels(a, l.m, ab), P = HalfMatrix::panels(b, l.m, ab);
     for (int k = 0; k < steps; ++k) {
-        const HalfMatrix X{x[k & 1], l.ld, 64, xb};
-        const OrthoSymmetric<false> gram{{}, nullptr, a, l.lda, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
+        const HalfMatrix X = HalfMatrix::panels(x[k & 1], rows, xb);
+        const OrthoSymmetric<false> gram{{}, nullptr, a, a_panel, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
         if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
                          : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))
             return MP8_ERR_HIP;
-        const OrthoSymmetric<true> poly{{}, a, b, l.lda, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+        const OrthoSymmetric<true> poly{{}, a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
         if (!ortho_product<false, false>(batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
         auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
             return rows <= cols ? ortho_product<false, true>(batch, P, X, rows, c8, l.m, false, skip_if_nonzero, epi, st)
                                 : ortho_product<false, false>(batch, X, P, rows, cols, l.m, false, skip_if_nonzero, epi, st);
         };
         const bool last = k + 1 == steps;
-        if (!last && !second(OrthoNext{{}, X.p, x[(k + 1) & 1], l.ld, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
-        if (last && !second(OrthoUpdate{{}, X.p, l.ld, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
+        if (!last && !second(OrthoNext{{}, X.p, x[(k + 1) & 1], x_panel, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
+        if (last && !second(OrthoUpdate{{}, X.p, x_panel, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
             return MP8_ERR_HIP;
     }
     return MP8_OK;

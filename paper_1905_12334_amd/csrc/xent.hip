@@ -199,7 +199,7 @@ struct XentError {
             lines.each([&](int r, int c, const u32x4 &v) {
                 const int row = at.row0 + 32 * i + r;
                 // (read again when it has left the caches: 8192 x 32768 x 2048 984 -> 958 us, in 128x128 tiles 1240 -> 1109)
-                if (row < M && at.col0 + c < wide) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + ((at.col0 + c) >> 6) * panel + 64 * row + ((at.col0 + c) & 63)));
+                if (row < M && at.col0 + c < wide) __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + HalfMatrix::at(row, at.col0 + c, panel)));
             });
         }
     }
@@ -300,11 +300,11 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
     }
 }
 
-// dst [rows, ld] halves <- src [rows, cols] halves or 8-bit codes, zeros beyond, TR threads per row; rows whose target is none are
+// dst <- src [rows, cols] halves or 8-bit codes, as halves in panels, zeros up to the `wide` columns of the last one, tr threads per row; rows whose target is none are
 // zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).  VEC: rows of
 // whole, aligned groups of eight.  factor, where given, becomes that of a call without token weights.
 template <bool CODES, bool VEC>
-__global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__ src, int64_t ld_src, uint16_t *__restrict__ dst, int64_t ld,
+__global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__ src, int64_t ld_src, uint16_t *__restrict__ dst, int wide,
                                                         int rows, int cols, const int64_t *__restrict__ targets, int N, int tr,
                                                         float *__restrict__ factor, int *__restrict__ exponent) {
     const int64_t r = (int64_t)blockIdx.x * (256 / tr) + threadIdx.x / tr;
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__
         factor[r] = live ? (float)(1 << kErrorExponent) : 0.0f;
         if (r == 0) *exponent = 0;
     }
-    for (int c = c0; c < ld; c += 8 * tr) {
+    for (int c = c0; c < wide; c += 8 * tr) {
         u32x4 o = {0, 0, 0, 0};
         if (live) {
             if (VEC) {
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__
                 }
             }
         }
-        *reinterpret_cast<u32x4 *>(dst + r * ld + c) = o;
+        *reinterpret_cast<u32x4 *>(dst + HalfMatrix::at(r, c, 64 * (int64_t)rows)) = o;
     }
 }
 
@@ -456,7 +456,7 @@ constexpr int64_t kPieceBytes = (int64_t)512 << 20;
 bool aligned_ld(int64_t K, int64_t ld) { return K % 8 == 0 && ld % 8 == 0; }
 
 Shape make_shape(int64_t M, int64_t N, int64_t K, bool copy_x, bool copy_w, bool backward) {
-    Shape s{M, N, K, half_pitch(K), copy_x, copy_w, N};
+    Shape s{M, N, K, up(K, 64), copy_x, copy_w, N};
     // bytes per class: of e and of the FP32 sums of dw, of a copy of w
     const int64_t row_e = backward ? (2 * M > 4 * s.Kp ? 2 * M : 4 * s.Kp) : 0, row_w = copy_w ? 2 * s.Kp : 0, row = row_e > row_w ? row_e : row_w;
     if (row) {
@@ -554,14 +554,15 @@ bool product(int tile, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, i
     return half_gemm_launch_plan<ATN, BTN>(tile, half_gemm_args(a, b, rows, cols, kc, tile, splits, false, 1), epi, stream);
 }
 
-bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t ld, int64_t rows, int64_t cols,
+bool copy_half(const void *src, bool codes, int64_t ld_src, uint16_t *dst, int64_t rows, int64_t cols,
                const int64_t *targets, int64_t N, float *factor, int *exponent, hipStream_t stream) {
+    const int64_t wide = up(cols, 64);
     int tr = 1;
-    while (tr < 256 && 8 * tr < ld) tr *= 2;
+    while (tr < 256 && 8 * tr < wide) tr *= 2;
     const bool vec = cols % 8 == 0 && ld_src % 8 == 0;
     const auto kernel = codes ? (vec ? xent_copy_kernel<true, true> : xent_copy_kernel<true, false>)
                               : (vec ? xent_copy_kernel<false, true> : xent_copy_kernel<false, false>);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / tr - 1) / (256 / tr))), dim3(256), 0, stream, src, ld_src, dst, ld, (int)rows, (int)cols,
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + 256 / tr - 1) / (256 / tr))), dim3(256), 0, stream, src, ld_src, dst, (int)wide, (int)rows, (int)cols,
                        targets, (int)N, tr, factor, exponent);
     return hipGetLastError() == hipSuccess;
 }
@@ -595,26 +596,22 @@ extern "C" mp8_status mp8_softmax_xent_fwd_fp16(int64_t M, int64_t N, int64_t K,
     if (!workspace || workspace_bytes < l.total) return MP8_ERR_WORKSPACE;
     uint8_t *ws = (uint8_t *)workspace;
     hipStream_t st = (hipStream_t)stream;
-    const uint16_t *xs = (const uint16_t *)x;
-    int64_t ld_x = ldx;
+    HalfMatrix X = HalfMatrix::rows((const uint16_t *)x, ldx);
     if (s.copy_x) {
-        xs = (uint16_t *)(ws + l.x);
-        if (!copy_half(x, x_is_e5m2 != 0, ldx, (uint16_t *)(ws + l.x), s.Kp, M, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
-        ld_x = s.Kp;
+        X = HalfMatrix::panels((uint16_t *)(ws + l.x), M);
+        if (!copy_half(x, x_is_e5m2 != 0, ldx, (uint16_t *)(ws + l.x), M, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
     }
     int parts = 0;
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
-        const uint16_t *wp = w + c * ldw;
-        int64_t ld_w = ldw;
+        HalfMatrix W = HalfMatrix::rows(w + c * ldw, ldw);
         if (s.copy_w) {
-            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
-            wp = (uint16_t *)(ws + l.w);
-            ld_w = s.Kp;
+            if (!copy_half(W.p, false, ldw, (uint16_t *)(ws + l.w), cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
+            W = HalfMatrix::panels((uint16_t *)(ws + l.w), cols);
         }
         const int tile = logits_plan(M, cols, K).tile;
         const XentStats epi{targets, (f32x2 *)(ws + l.part), (float *)(ws + l.z_target), (int)M, (int)cols, (int)c, parts};
-        if (!product<false, false>(tile, HalfMatrix::rows(xs, ld_x), HalfMatrix::rows(wp, ld_w), M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
+        if (!product<false, false>(tile, X, W, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
         parts += (int)((cols + tile - 1) / tile);
     }
     const int per = M >= 512 ? 8 : 1;
@@ -648,13 +645,13 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     uint16_t *xs = (uint16_t *)(ws + l.x), *e = (uint16_t *)(ws + l.e);
     float *factor = (float *)(ws + l.factor), *dxs = (float *)(ws + l.dx), *dws = (float *)(ws + l.dw);
     int *exponent = (int *)(ws + l.exponent);
-    if (!copy_half(x, x_is_e5m2 != 0, ldx, xs, s.Kp, M, K, targets, N, dloss ? nullptr : factor, exponent, st)) return MP8_ERR_HIP;
+    if (!copy_half(x, x_is_e5m2 != 0, ldx, xs, M, K, targets, N, dloss ? nullptr : factor, exponent, st)) return MP8_ERR_HIP;
     if (dloss) {
         hipLaunchKernelGGL(xent_factor_kernel, dim3(1), dim3(1024), 0, st, targets, dloss, factor, exponent, (int)M, (int)N);
         if (hipGetLastError() != hipSuccess) return MP8_ERR_HIP;
     }
     const int64_t K8 = up(K, 8);
-    const HalfMatrix E = HalfMatrix::panels(e, M), X = HalfMatrix::rows(xs, s.Kp);
+    const HalfMatrix E = HalfMatrix::panels(e, M), X = HalfMatrix::panels(xs, M);
     const BwdPlans plans = bwd_plans(s);
     auto finish = [&](const float *sum, int64_t slab, int slabs, int64_t rows, int64_t row0, uint16_t *out16, uint8_t *out8, uint64_t offset,
                       mp8_stats *stats) {
@@ -676,14 +673,11 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     };
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
-        const uint16_t *wp = w + c * ldw;
-        int64_t ld_w = ldw;
+        HalfMatrix W = HalfMatrix::rows(w + c * ldw, ldw);
         if (s.copy_w) {
-            if (!copy_half(wp, false, ldw, (uint16_t *)(ws + l.w), s.Kp, cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
-            wp = (uint16_t *)(ws + l.w);
-            ld_w = s.Kp;
+            if (!copy_half(W.p, false, ldw, (uint16_t *)(ws + l.w), cols, K, nullptr, N, nullptr, nullptr, st)) return MP8_ERR_HIP;
+            W = HalfMatrix::panels((uint16_t *)(ws + l.w), cols);
         }
-        const HalfMatrix W = HalfMatrix::rows(wp, ld_w);
         const XentError epi{targets, loss, lse, factor, e, E.panel, (int)up(cols, 64), (int)M, (int)cols, (int)c};
         if (!product<false, false>(logits_plan(M, cols, K).tile, X, W, M, cols, K, 1, epi, st)) return MP8_ERR_HIP;
         if (dx) {
