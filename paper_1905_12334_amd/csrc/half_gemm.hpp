@@ -32,6 +32,10 @@ struct HalfGemm {
     int symmetric;       // square output of which only the tiles on and above the diagonal are made
     const uint32_t *skip;  // nullable: a call that is skipped if this is not zero
     uint32_t total;        // tiles of all slices and batches
+    // A sliced contraction whose epilogue wants the whole sum (Epi::kJoin): every slice's tile goes to `parts`, and the workgroup that finds
+    // in `arrived` (one word per tile, zero before and after the call) that it is the last one adds them up, in the order of the slices.
+    float *parts;
+    uint32_t *arrived;
     FastDiv div_tiles;   // by the tiles of one slice
     FastDiv div_splits;
     FastDiv div_band, div_last, div_tn;  // by 8 * tiles_n, by the height of the last band of 8 tile rows, by tiles_n
@@ -40,6 +44,7 @@ struct HalfGemm {
 // Which part of the output a workgroup makes.
 struct HalfTile {
     int batch, split, tm, tn;
+    uint32_t tile;  // among those of its batch
 };
 
 // Consecutive workgroups go to different XCDs, each with an L2 of its own: number i is the i/8-th tile of the i%8-th eighth of
@@ -52,6 +57,7 @@ __device__ __forceinline__ HalfTile half_tile(const HalfGemm &p) {
     id = fastdiv(id, p.div_tiles, tile);
     t.batch = (int)fastdiv(id, p.div_splits, split);
     t.split = (int)split;
+    t.tile = tile;
     if (p.symmetric) {
         // row i of the upper triangle starts at i (2 T - i + 1) / 2; counted from the end, row T - 1 - k has k + 1 tiles
         const uint32_t T = (uint32_t)p.tiles_m, back = T * (T + 1) / 2 - 1 - tile;
@@ -404,6 +410,57 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
         for (; t + 1 < ks_count; ++t) stage(t, std::false_type{}, std::true_type{});
         if (t < ks_count) stage(t, std::false_type{}, std::false_type{});
     }
+    if constexpr (Epi::kJoin) {
+        if (p.splits > 1) {
+            constexpr int PART = BM * BN / 4;  // groups of four floats of a tile, as the lanes hold them
+            const uint32_t place = (uint32_t)tile.batch * p.div_tiles.d + (uint32_t)__builtin_amdgcn_readfirstlane((int)tile.tile);
+            f32x4 *parts = reinterpret_cast<f32x4 *>(p.parts) + (int64_t)place * p.splits * PART + wave * (PART / 4) + lane;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        store_through(parts + (int64_t)tile.split * PART + ((i * NT + j) * 4 + g) * 64,
+                                      f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+            // Stores and loads of agent scope go past the XCDs' L2 caches, and a store that has been waited for has arrived: no cache has to
+            // be written back or emptied, as an acquiring and releasing counter would have it (4 us of 7 for 128 x 128 x 1152).
+            wait_vm_lds<0>();
+            __syncthreads();
+            uint32_t *last = reinterpret_cast<uint32_t *>(lds);
+            if (threadIdx.x == 0) {
+                const uint32_t before = __hip_atomic_fetch_add(p.arrived + place, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                *last = before + 1u == (uint32_t)p.splits ? 1u : 0u;
+                if (*last) __hip_atomic_store(p.arrived + place, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            if (*last == 0u) return;
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            constexpr int N = MT * NT * 4, U = N == 4 ? 8 : 1;  // loads of a slice, slices under way together
+            for (int s0 = 0; s0 < p.splits; s0 += U) {
+                u32x4 v[U][N];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        v[u][n] = s0 + u < p.splits
+                                      ? __builtin_amdgcn_global_load_b128((__attribute__((address_space(1))) u32x4 *)(parts + (int64_t)(s0 + u) * PART + n * 64), "agent")
+                                      : u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[n / 4 / NT][n / 4 % NT][4 * (n % 4) + e] += u2f(v[u][n][e]);
+            }
+        }
+    }
     epi(at, acc, ahead);
 }
 
@@ -504,6 +561,7 @@ __device__ __forceinline__ u32x4 half_round8(const float v[8]) {
 }
 
 struct HalfNoneAhead {
+    static constexpr bool kJoin = false;
     template <class P>
     __device__ __forceinline__ HalfNothing ahead(const P &) const { return {}; }
 };
@@ -559,8 +617,8 @@ static inline double half_cost(int tile, int64_t tiles, double stages) {
 // Few 64x64 tiles over a long contraction: kByIndex (the waves' sums cost 1 us, a stage 0.08 us less).
 static inline bool half_by_index(int64_t tiles, double stages) { return tiles <= 256 && stages >= 14; }
 
-// most_splits > 1: the slices' FP32 sums are written and added up by a pass of its own.
-static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int64_t kc, bool symmetric, int most_splits) {
+// most_splits > 1: the slices' FP32 sums are written and added up, by a pass of its own or (joined) by the last workgroup of every tile.
+static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int64_t kc, bool symmetric, int most_splits, bool joined = false) {
     HalfPlan best{64, 1};
     double least = 1e300;
     for (const int tile : {256, 192, 128, 64}) {
@@ -568,8 +626,11 @@ static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int6
         const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn), steps = (kc + 63) / 64;
         if (tiles > (int64_t)1 << 23) continue;
         for (int s = 1; s <= most_splits && s <= steps; s = s < 8 ? s + 1 : s + s / 4) {
-            // (slices of one more pass: 4 bytes out and in again per element and slice, at 4 TB/s)
-            const double t = half_cost(tile, tiles * s, (double)((steps + s - 1) / s)) + (s > 1 ? 2.0e-6 * (double)(batch * rows * cols) * s : 0.0);
+            // slices of one more pass: 4 bytes out and in again per element and slice, at 4 TB/s; joined: a tile's out
+            // and in of one CU (measured on Gram products: 128 x 128 x 1152 in 6 slices 7.0 us, unsplit 9.3; 1024 x 1024 x 4096 14.2 and 16.4)
+            const double more = s == 1 ? 0.0 : joined ? 1.5 + 4.0e-6 * (double)(tile * tile) * s * 4.0 + 1.0e-6 * (double)(tiles * tile * tile) * s
+                                                      : 2.0e-6 * (double)(batch * rows * cols) * s;
+            const double t = half_cost(tile, tiles * s, (double)((steps + s - 1) / s)) + more;
             if (t < least) {
                 least = t;
                 best = {tile, s};

@@ -37,6 +37,7 @@ __device__ __forceinline__ u32x4 ortho_combine(float linear, const u32x4 &x, flo
 // With the conversions of the results' epilogues (canonical NaN, a test per element) two bands of a 128x128 tile took 5 us.
 template <bool POLY>
 struct OrthoSymmetric : HalfNoneAhead {
+    static constexpr bool kJoin = !POLY;
     const uint16_t *in;
     uint16_t *out;
     int64_t panel, batch;  // in halves
@@ -203,11 +204,15 @@ struct OrthoMomentum {
     const uint32_t *skip;
     double *squares;  // [batch, blocks]
     mp8_stats *stats;
+    uint32_t *arrived;  // `words` of them become zero (HalfGemm::arrived)
+    int words;
 };
 __device__ __forceinline__ float ortho_direction(float v, float g, float mu, int nesterov) { return nesterov ? __builtin_fmaf(mu, v, g) : v; }
 
 __global__ __launch_bounds__(256) void ortho_momentum_kernel(const OrthoMomentum p) {
     __shared__ double sh[4];
+    if (blockIdx.y == 0)
+        for (int i = blockIdx.x * 256 + threadIdx.x; i < p.words; i += gridDim.x * 256) p.arrived[i] = 0u;
     const bool skipping = p.skip != nullptr && *p.skip != 0u;
     if (skipping && p.stats == nullptr) return;
     const int64_t base = (int64_t)blockIdx.y * p.n;
@@ -328,7 +333,9 @@ int64_t up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct OrthoLayout {
     int64_t m, n, x_batch, a_batch;  // shorter and longer side; halves of an X and of an A
     int blocks;             // workgroups of the momentum pass per matrix
-    size_t squares, x0, x1, a, b, total;
+    HalfPlan gram;
+    int64_t words;          // tiles of the Gram matrices
+    size_t squares, x0, x1, a, b, parts, arrived, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     OrthoLayout l{};
@@ -338,6 +345,9 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     l.a_batch = l.m * up(l.m, 64);
     const int64_t want = (rows * cols + 4095) / 4096, most = batch >= 256 ? 4 : 1024 / batch;
     l.blocks = (int)(want < 1 ? 1 : want > most ? most : want);
+    l.gram = half_plan(batch, l.m, l.m, l.n, true, 32, true);
+    const int64_t t = (l.m + l.gram.tile - 1) / l.gram.tile;
+    l.words = l.gram.splits > 1 ? batch * (t * (t + 1) / 2) : 0;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
@@ -349,6 +359,8 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     l.x1 = take(2 * batch * l.x_batch);
     l.a = take(2 * batch * l.a_batch);
     l.b = take(2 * batch * l.a_batch);
+    l.parts = take(4 * l.words * l.gram.splits * l.gram.tile * l.gram.tile);
+    l.arrived = take(4 * l.words);
     l.total = at;
     return l;
 }
@@ -364,12 +376,13 @@ mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
 }
 
 template <bool ATN, bool BTN, class Epi>
-bool ortho_product(int64_t batch, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t cols, int64_t kc, bool symmetric,
-                   const uint32_t *skip, const Epi &epi, hipStream_t stream) {
-    const int tile = half_plan(batch, rows, cols, kc, symmetric, 1).tile;
-    HalfGemm p = half_gemm_args(a, b, rows, cols, kc, tile, 1, symmetric, batch);
+bool ortho_product(const HalfPlan &plan, int64_t batch, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t cols, int64_t kc, bool symmetric,
+                   const uint32_t *skip, float *parts, uint32_t *arrived, const Epi &epi, hipStream_t stream) {
+    HalfGemm p = half_gemm_args(a, b, rows, cols, kc, plan.tile, plan.splits, symmetric, batch);
     p.skip = skip;
-    return half_gemm_launch_plan<ATN, BTN>(tile, p, epi, stream);
+    p.parts = parts;
+    p.arrived = arrived;
+    return half_gemm_launch_plan<ATN, BTN>(plan.tile, p, epi, stream);
 }
 
 }  // namespace
@@ -402,10 +415,12 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     hipStream_t st = (hipStream_t)stream;
     double *squares = (double *)(ws + l.squares);
     uint16_t *x[2] = {(uint16_t *)(ws + l.x0), (uint16_t *)(ws + l.x1)}, *a = (uint16_t *)(ws + l.a), *b = (uint16_t *)(ws + l.b);
+    float *parts = (float *)(ws + l.parts);
+    uint32_t *arrived = (uint32_t *)(ws + l.arrived);
     const double s = std::exp2(std::nearbyint(0.5 * std::log2((double)l.n)));
     const auto ok = [] { return hipGetLastError() == hipSuccess; };
 
-    const OrthoMomentum mom{velocity, g8, rows * cols, inv_loss_scale, momentum, nesterov, l.blocks, skip_if_nonzero, squares, stats};
+    const OrthoMomentum mom{velocity, g8, rows * cols, inv_loss_scale, momentum, nesterov, l.blocks, skip_if_nonzero, squares, stats, arrived, (int)l.words};
     hipLaunchKernelGGL(ortho_momentum_kernel, dim3((unsigned)l.blocks, (unsigned)batch), dim3(256), 0, st, mom);
     if (!ok()) return MP8_ERR_HIP;
     const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = l.x_batch, ab = l.a_batch, x_panel = 64 * rows, a_panel = 64 * l.m;
@@ -418,14 +433,16 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     for (int k = 0; k < steps; ++k) {
         const HalfMatrix X = HalfMatrix::panels(x[k & 1], rows, xb);
         const OrthoSymmetric<false> gram{{}, nullptr, a, a_panel, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
-        if (rows <= cols ? !ortho_product<false, false>(batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, gram, st)
-                         : !ortho_product<true, true>(batch, X, X, m8, m8, l.n, true, skip_if_nonzero, gram, st))
+        if (rows <= cols ? !ortho_product<false, false>(l.gram, batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, parts, arrived, gram, st)
+                         : !ortho_product<true, true>(l.gram, batch, X, X, m8, m8, l.n, true, skip_if_nonzero, parts, arrived, gram, st))
             return MP8_ERR_HIP;
         const OrthoSymmetric<true> poly{{}, a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
-        if (!ortho_product<false, false>(batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, poly, st)) return MP8_ERR_HIP;
+        if (!ortho_product<false, false>(half_plan(batch, l.m, l.m, l.m, true, 1), batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, nullptr, nullptr, poly, st))
+            return MP8_ERR_HIP;
         auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
-            return rows <= cols ? ortho_product<false, true>(batch, P, X, rows, c8, l.m, false, skip_if_nonzero, epi, st)
-                                : ortho_product<false, false>(batch, X, P, rows, cols, l.m, false, skip_if_nonzero, epi, st);
+            const HalfPlan plan = half_plan(batch, rows, cols, l.m, false, 1);
+            return rows <= cols ? ortho_product<false, true>(plan, batch, P, X, rows, c8, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st)
+                                : ortho_product<false, false>(plan, batch, X, P, rows, cols, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st);
         };
         const bool last = k + 1 == steps;
         if (!last && !second(OrthoNext{{}, X.p, x[(k + 1) & 1], x_panel, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
