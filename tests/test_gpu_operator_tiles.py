@@ -1,0 +1,280 @@
+"""GPU tests of the softmax cross entropy and the orthogonalised momentum at sizes that fill the larger tiles, cut contractions and the
+vocabulary into pieces and leave odd edges, against their definitions in 64 bits (on the GPU, in torch), and of a training step in which
+both are used together with the 8-bit layers.  Tolerances as derived in test_gpu_softmax_xent.py and test_gpu_orthogonal_momentum.py."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U, H = 2.0 ** -24, 2.0 ** -11
+A, B, C = 3.4445, -4.7750, 2.0315
+
+
+@pytest.fixture(scope="module")
+def mp8():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    import paper_1905_12334_amd as m
+    m.lib()
+    return m
+
+
+def codes(x):
+    return x.float().to(torch.float8_e5m2).view(torch.uint8)
+
+
+def values(c):
+    return c.view(torch.float8_e5m2).double()
+
+
+def bytes_of(n):
+    return torch.full((max(n, 16),), 0xFF, dtype=torch.uint8, device="cuda")
+
+
+# ------------------------------------------------------------------ softmax cross entropy
+def truth(x, w, t, scale):
+    """Results in 64 bits and the elementwise bounds."""
+    (M, K), N = x.shape, w.shape[0]
+    live = (t >= 0) & (t < N)
+    at, rows = torch.where(live, t, 0), torch.arange(M, device="cuda")
+    z = x @ w.t()
+    dz = K * U * (x.abs() @ w.abs().t()).amax(1)
+    lse = torch.logsumexp(z, 1)
+    spread = (z.amax(1) - z.amin(1)) / math.log(2) + 1
+    r = 2 * dz + (math.log(2) * spread + 64 + N / 32 + 16) * U
+    others = torch.exp(z - z[rows, at][:, None])
+    others[rows, at] = 0
+    loss = torch.where(live, torch.log1p(others.sum(1)), 0.0)
+    del others
+    e = torch.exp(z - lse[:, None])
+    e[rows[live], t[live]] = torch.expm1(-loss[live])
+    e = torch.where(live[:, None], e, 0.0) * scale
+    r = torch.where(live, r, 0.0)
+    de = (H + r + 8 * U)[:, None] * e.abs() + torch.where(live, 2.0 ** -39 * scale, 0.0)[:, None]
+    dx, dw = e @ w, e.t() @ x
+    bx, bw = de @ w.abs() + N * U * (e.abs() @ w.abs()), de.t() @ x.abs() + M * U * (e.abs().t() @ x.abs())
+    return dict(loss=loss, lse=lse, r=r, dlse=r + 4 * U * lse.abs(), dx=dx, dw=dw, bx=bx, bw=bw, live=live)
+
+
+def inputs(seed, M, N, K):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    w = (torch.randn((N, K), generator=gen, device="cuda") * K ** -0.5).half()
+    t = torch.randint(0, N, (M,), generator=gen, device="cuda")
+    x = (torch.randn((M, K), generator=gen, device="cuda") + 4 * torch.rand((M, 1), generator=gen, device="cuda") * w[t].float()).half()
+    t[torch.rand(M, generator=gen, device="cuda") < 0.1] = -100
+    return x, w, t
+
+
+def within(got, want, bound, what):
+    off = (got.double().view_as(want) - want).abs()
+    assert bool((off <= bound).all()), (what, float((off / bound).max()))
+
+
+@pytest.mark.parametrize("M,N,K", [(2055, 4099, 136), (3001, 9001, 72), (4099, 8200, 520), (1111, 40009, 264), (9001, 1999, 1032), (512, 20001, 2056),
+                                   (8200, 40001, 40)])
+def test_cross_entropy_of_large_tiles(mp8, M, N, K):
+    x, w, t = inputs(M + N, M, N, K)
+    scale = 256.0 / M
+    want = truth(x.double(), w.double(), t, scale)
+    loss, lse = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    mp8.softmax_xent_fwd_fp16(M, N, K, x, w, t, loss, lse, workspace=bytes_of(mp8.softmax_xent_fwd_workspace_bytes(M, N, K)))
+    within(lse, want["lse"], want["dlse"], "lse")
+    within(loss, want["loss"], want["loss"] * (want["r"] + 4 * U) + 1e-44, "loss")
+    ws = bytes_of(mp8.softmax_xent_bwd_workspace_bytes(M, N, K))
+    dx, dw = torch.full((M * K + 64,), 7.0, dtype=torch.float16, device="cuda"), torch.full((N * K + 64,), 7.0, dtype=torch.float16, device="cuda")
+    sx, sw = mp8.new_stats(), mp8.new_stats()
+    mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dx16=dx[:M * K], dw16=dw[:N * K], scale=scale, dx_stats=sx, dw_stats=sw, workspace=ws)
+    assert bool((dx[M * K:] == 7).all()) and bool((dw[N * K:] == 7).all())
+    for got, key, n, stats in ((dx, "x", M * K, sx), (dw, "w", N * K, sw)):
+        value, bound = want["d" + key], want["b" + key]
+        within(got[:n], value, bound + H * (value.abs() + bound) + 2.0 ** -25, "d" + key)
+        assert float((got[:n].double().view_as(value) - value).norm() / value.norm()) <= H
+        amax, bad, _ = mp8.read_stats(stats)
+        top = torch.tensor([amax], dtype=torch.int32).view(torch.float32)
+        assert bad == 0 and abs(float(top) - float(value.abs().max())) <= float(bound.max())
+    # codes, alone and beside the halves, which stay the same
+    for sr in (False, True):
+        cx, cw = torch.full((M * K + 64,), 0xAA, dtype=torch.uint8, device="cuda"), torch.full((N * K + 64,), 0xAA, dtype=torch.uint8, device="cuda")
+        ax, aw = torch.empty_like(x), torch.empty_like(w)
+        kw = dict(scale=scale, round=mp8.SR if sr else mp8.RNE, seed=5, dx_offset=1, dw_offset=2)
+        mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dx8=cx[:M * K], dw8=cw[:N * K], dx16=ax, dw16=aw, workspace=ws, **kw)
+        assert torch.equal(ax.view(-1), dx[:M * K]) and torch.equal(aw.view(-1), dw[:N * K])
+        assert bool((cx[M * K:] == 0xAA).all()) and bool((cw[N * K:] == 0xAA).all())
+        for got, key, n in ((cx, "x", M * K), (cw, "w", N * K)):
+            # a step of a value is 2^-2 of its power of two; subnormal steps are 2^-16
+            value, bound = want["d" + key], want["b" + key]
+            step = torch.maximum(torch.exp2(torch.floor(torch.log2(value.abs() + bound))) / 4, torch.tensor(2.0 ** -16, device="cuda"))
+            within(values(got[:n]), value, bound + step * (1.0 if sr else 0.5), "code of d" + key)
+        only = torch.empty(N * K, dtype=torch.uint8, device="cuda")
+        mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dw8=only, workspace=ws, **kw)
+        assert torch.equal(only, cw[:N * K])
+        only = torch.empty(M * K, dtype=torch.uint8, device="cuda")
+        mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dx8=only, workspace=ws, **kw)
+        assert torch.equal(only, cx[:M * K])
+
+
+# ------------------------------------------------------------------ orthogonalised momentum
+def iterate(u, steps, rounded):
+    """X after `steps`; `rounded`: with the operands rounded to half as stored (X times s, A and the polynomial times 2^14)."""
+    tall = u.shape[0] > u.shape[1]
+    u = u.t().contiguous() if tall else u
+    x = u / u.norm()
+    s = 2.0 ** round(0.5 * math.log2(u.shape[1]))
+    half = (lambda v, f: (v * f).half().double() / f) if rounded else (lambda v, f: v)
+    x = half(x, s)
+    for k in range(steps):
+        a = half(x @ x.t().contiguous(), 2.0 ** 14)
+        p = half(B * a + C * (a @ a), 2.0 ** 14)
+        x = A * x + p @ x
+        if k + 1 < steps:
+            x = half(x, s)
+    return x.t().contiguous() if tall else x
+
+
+def momentum(mp8, w, v, g, lr, **kw):
+    batch = w.numel() // (w.shape[-1] * w.shape[-2])
+    ws = bytes_of(mp8.orthogonal_momentum_workspace_bytes(batch, *w.shape[-2:]))
+    mp8.orthogonal_momentum_fp16_sr(w, v, g, lr, 1.0, 0.9, round=mp8.RNE, workspace=ws, **kw)
+
+
+@pytest.mark.parametrize("batch,rows,cols", [
+    (1, 40, 8192), (1, 8192, 40), (5, 30, 2100), (3, 3001, 65), (2, 100, 5000), (1, 1, 20000), (1, 129, 30001), (1, 260, 8192), (1, 1024, 1024),
+    (1, 1001, 1003), (9, 500, 520), (20, 257, 389), (1, 1500, 1499), (1, 2049, 2560), (2, 2100, 4099), (1, 4100, 3700), (1, 700, 20011), (1, 20011, 700),
+    (1, 4104, 6200)])
+def test_direction_of_large_tiles(mp8, batch, rows, cols):
+    gen = torch.Generator(device="cuda").manual_seed(rows + cols)
+    g = codes(torch.randn((batch, rows, cols), generator=gen, device="cuda"))
+    v = torch.zeros((batch, rows, cols), device="cuda")
+    n = batch * rows * cols
+    w = torch.zeros(n + 64, dtype=torch.float16, device="cuda")
+    w[n:] = 7
+    momentum(mp8, w[:n].view(batch, rows, cols), v, g, -1.0, nesterov=False)
+    assert torch.equal(v.double(), values(g)) and bool((w[n:] == 7).all())
+    got = w[:n].view(batch, rows, cols)
+    for i in {0, batch - 1}:
+        u = v[i].double()
+        exact, model = iterate(u, 5, False), iterate(u, 5, True)
+        assert float((got[i].double() - exact).norm()) <= float(2 * (model - exact).norm() + H * exact.norm())
+    # again, the same bits: what is added in several parts is added in their order
+    again, v2 = torch.zeros_like(got), torch.zeros_like(v)
+    momentum(mp8, again, v2, g, -1.0, nesterov=False)
+    assert torch.equal(again, got)
+
+
+def test_two_momentum_calls_at_once_on_two_streams(mp8):
+    shapes = [(1, 128, 6000), (4, 300, 400)]
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    data = [(torch.randn(s, generator=gen, device="cuda"), codes(torch.randn(s, generator=gen, device="cuda"))) for s in shapes]
+    want = []
+    for v, g in data:
+        w = torch.zeros(v.shape, dtype=torch.float16, device="cuda")
+        v = v.clone()
+        momentum(mp8, w, v, g, -1.0)
+        want.append((w, v))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in shapes]
+    for _ in range(3):
+        got = []
+        for (v, g), s in zip(data, streams):
+            with torch.cuda.stream(s):
+                w, v = torch.zeros(v.shape, dtype=torch.float16, device="cuda"), v.clone()
+                momentum(mp8, w, v, g, -1.0)
+                got.append((w, v))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+# ------------------------------------------------------------------ together
+class Step:
+    """A training step: an 8-bit layer, ReLU on the codes, a last layer in FP16 with the cross entropy, the layer's weights by
+    orthogonalised momentum, the last layer's by plain momentum, both left out where a gradient overflowed."""
+
+    def __init__(self, mp8, M=1008, D=264, K=520, N=3001):
+        self.mp8, self.M, self.D, self.K, self.N = mp8, M, D, K, N
+        gen = torch.Generator(device="cuda").manual_seed(7)
+        u8, dev = torch.uint8, "cuda"
+        empty = lambda *s, d=u8: torch.empty(s, dtype=d, device=dev)
+        self.x8 = codes(torch.randn((M, D), generator=gen, device=dev))
+        self.t = torch.randint(0, N, (M,), generator=gen, device=dev)
+        self.t[::17] = -100
+        self.w1 = (torch.randn((K, D), generator=gen, device=dev) * (2 / D) ** 0.5).half()
+        self.w2 = (torch.randn((N, K), generator=gen, device=dev) * K ** -0.5).half()
+        self.w1_8 = codes(self.w1)
+        self.v1, self.v2 = torch.zeros((K, D), device=dev), torch.zeros((N, K), device=dev)
+        self.h8, self.r8, self.dr8, self.dh8, self.g1, self.g2 = empty(M, K), empty(M, K), empty(M, K), empty(M, K), empty(K, D), empty(N, K)
+        self.loss, self.lse = empty(M, d=torch.float32), empty(M, d=torch.float32)
+        self.stats = mp8.new_stats()
+        need = max(mp8.softmax_xent_fwd_workspace_bytes(M, N, K), mp8.softmax_xent_bwd_workspace_bytes(M, N, K),
+                   mp8.orthogonal_momentum_workspace_bytes(1, K, D), 64 << 20)
+        self.ws = empty(need)
+
+    def state(self):
+        return [a.clone() for a in (self.w1, self.w2, self.w1_8, self.v1, self.v2, self.loss, self.g1, self.g2)]
+
+    def run(self, loss_scale, lr=0.02):
+        m, M, D, K, N = self.mp8, self.M, self.D, self.K, self.N
+        scale = loss_scale / M
+        m.gemm_fp8(m.FWD, M, K, D, self.x8, self.w1_8, out8=self.h8, workspace=self.ws)
+        torch.mul(self.h8, self.h8 < 0x80, out=self.r8)
+        m.softmax_xent_fwd_fp16(M, N, K, self.r8, self.w2, self.t, self.loss, self.lse, workspace=self.ws)
+        self.stats.zero_()
+        m.softmax_xent_bwd_fp16(M, N, K, self.r8, self.w2, self.t, self.loss, self.lse, dx8=self.dr8, dw8=self.g2, scale=scale,
+                                dx_stats=self.stats, dw_stats=self.stats, workspace=self.ws)
+        torch.mul(self.dr8, self.r8 != 0, out=self.dh8)
+        m.gemm_fp8(m.WGRAD, M, D, K, self.dh8, self.x8, out8=self.g1, stats=self.stats, workspace=self.ws, flags=m.FLAG_CONTRACTION_MAJOR)
+        bad = self.stats.view(torch.int32)[1:2]
+        m.orthogonal_momentum_fp16_sr(self.w1, self.v1, self.g1, lr, 1.0 / loss_scale, 0.9, seed=3, offset=1, skip_if_nonzero=bad, w8_out=self.w1_8,
+                                      workspace=self.ws)
+        m.sgd_momentum_fp16_sr(self.w2, self.v2, self.g2, lr, 1.0 / loss_scale, 0.9, seed=3, offset=2, skip_if_nonzero=bad)
+
+
+def half_step(v):
+    """Half a step of the 8-bit format at |v|: 2^-3 of it at most, 2^-17 below the smallest normal value."""
+    return 2.0 ** -3 * v.abs() + 2.0 ** -17
+
+
+def test_a_training_step_with_both(mp8):
+    s = Step(mp8)
+    w1, w2, loss_scale, lr = s.w1.clone(), s.w2.clone(), 256.0, 0.02
+    s.run(loss_scale, lr)
+    want = truth(values(s.r8), w2.double(), s.t, loss_scale / s.M)
+    within(s.loss, want["loss"], want["loss"] * (want["r"] + 4 * U) + 1e-44, "loss")
+    within(values(s.dr8), want["dx"], want["bx"] + half_step(want["dx"].abs() + want["bx"]), "dx")
+    within(values(s.g2), want["dw"], want["bw"] + half_step(want["dw"].abs() + want["bw"]), "dw")
+    # through the first layer: what the codes of dx may be off by, the product's FP32 sums, one rounding
+    on, x = (s.r8 != 0).double(), values(s.x8)
+    dx, off = want["dx"] * on, (want["bx"] + half_step(want["dx"].abs() + want["bx"])) * on
+    g = dx.t() @ x
+    bound = off.t() @ x.abs() + s.M * U * ((dx.abs() + off).t() @ x.abs())
+    within(values(s.g1), g, bound + half_step(g.abs() + bound), "gradient of the first layer")
+    # the first layer's update: direction, stochastic rounding (less than a step, 2^-10), the 8-bit copy
+    assert torch.equal(s.v1.double(), values(s.g1) / loss_scale)
+    u = values(s.g1) * 1.9 / loss_scale
+    exact, model = iterate(u, 5, False), iterate(u, 5, True)
+    new = w1.double() - lr * exact
+    slack = lr * (2 * (model - exact).norm() + H * exact.norm()) + 2.0 ** -10 * new.norm()
+    assert float((s.w1.double() - new).norm()) <= float(slack)
+    assert torch.equal(s.w1_8, codes(s.w1)) and not torch.equal(s.w2, w2)
+
+
+def test_captured_training_steps_and_one_that_overflows(mp8):
+    eager, captured = Step(mp8), Step(mp8)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured.run(256.0)
+    for _ in range(4):
+        captured.ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager.ws.fill_(0xAA)
+        eager.run(256.0)
+        torch.cuda.synchronize()
+        for a, b in zip(captured.state(), eager.state()):
+            assert torch.equal(a, b)
+        assert mp8.read_stats(eager.stats)[1] == 0
+    before = eager.state()
+    eager.run(2.0 ** 40)
+    assert mp8.read_stats(eager.stats)[1] > 0
+    for a, b in zip(before[:5], eager.state()):
+        assert torch.equal(a, b)
