@@ -561,7 +561,7 @@ __device__ __forceinline__ u32x4 half_round8(const float v[8]) {
 }
 
 struct HalfNoneAhead {
-    static constexpr bool kJoin = false;
+    static constexpr bool kJoin = false, k192 = true;  // k192: plans may hold 192x192 tiles
     template <class P>
     __device__ __forceinline__ HalfNothing ahead(const P &) const { return {}; }
 };
@@ -682,7 +682,9 @@ static inline bool half_gemm_launch(const HalfGemm &p, const Epi &epi, hipStream
 template <bool ATN, bool BTN, class Epi>
 static inline bool half_gemm_launch_plan(int tile, const HalfGemm &p, const Epi &epi, hipStream_t stream) {
     if (tile == 256) return half_gemm_launch<Half256, ATN, BTN>(p, epi, stream);
-    if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, epi, stream);
+    if constexpr (Epi::k192) {
+        if (tile == 192) return half_gemm_launch<Half192, ATN, BTN>(p, epi, stream);
+    }
     if (tile == 128) return half_gemm_launch<Half128, ATN, BTN>(p, epi, stream);
     if (half_by_index(p.total, (double)p.ks_per)) return half_gemm_launch<Half64Few, ATN, BTN>(p, epi, stream);
     return half_gemm_launch<Half64, ATN, BTN>(p, epi, stream);

@@ -41,7 +41,7 @@ __device__ __forceinline__ int xent_column(int64_t target, int64_t first, int le
 }
 
 struct XentStats {
-    static constexpr bool kJoin = false;
+    static constexpr bool kJoin = false, k192 = false;  // (logits_plan)
     const int64_t *targets;
     f32x2 *part;     // [parts, M]: (B, sum) of the columns of one tile, without the target
     float *z_target; // [M]
@@ -129,7 +129,7 @@ struct XentStats {
 // e of a tile, as halves times 2^14 and the token's weight.
 using half4 = _Float16 __attribute__((ext_vector_type(4)));
 struct XentError {
-    static constexpr bool kJoin = false;
+    static constexpr bool kJoin = false, k192 = false;  // (logits_plan)
     const int64_t *targets;
     const float *loss, *lse, *factor;  // factor [M]: 2^14 and the token's weight; 0 without a target
     uint16_t *out;                     // panels of 64 columns, `wide` columns in all

@@ -49,11 +49,12 @@ def truth(x, w, t, scale):
     e = torch.exp(z - lse[:, None])
     e[rows[live], t[live]] = torch.expm1(-loss[live])
     e = torch.where(live[:, None], e, 0.0) * scale
+    dlse = r + 4 * U * lse.abs()  # (of tokens without a target too)
     r = torch.where(live, r, 0.0)
     de = (H + r + 8 * U)[:, None] * e.abs() + torch.where(live, 2.0 ** -39 * scale, 0.0)[:, None]
     dx, dw = e @ w, e.t() @ x
     bx, bw = de @ w.abs() + N * U * (e.abs() @ w.abs()), de.t() @ x.abs() + M * U * (e.abs().t() @ x.abs())
-    return dict(loss=loss, lse=lse, r=r, dlse=r + 4 * U * lse.abs(), dx=dx, dw=dw, bx=bx, bw=bw, live=live)
+    return dict(loss=loss, lse=lse, r=r, dlse=dlse, dx=dx, dw=dw, bx=bx, bw=bw, live=live)
 
 
 def inputs(seed, M, N, K):
@@ -71,7 +72,9 @@ def within(got, want, bound, what):
 
 
 @pytest.mark.parametrize("M,N,K", [(2055, 4099, 136), (3001, 9001, 72), (4099, 8200, 520), (1111, 40009, 264), (9001, 1999, 1032), (512, 20001, 2056),
-                                   (8200, 40001, 40)])
+                                   (8200, 40001, 40), (921, 16507, 386), (893, 18915, 472), (1, 34847, 136), (1, 36418, 135), (1215, 14131, 16),
+                                   (22139, 2, 2032), (15981, 937, 16), (33505, 2, 8), (37658, 2, 144), (34686, 756, 256), (1, 76922, 1), (35368, 2, 1),
+                                   (21873, 2, 324), (33885, 858, 194)])
 def test_cross_entropy_of_large_tiles(mp8, M, N, K):
     x, w, t = inputs(M + N, M, N, K)
     scale = 256.0 / M
@@ -88,7 +91,8 @@ def test_cross_entropy_of_large_tiles(mp8, M, N, K):
     for got, key, n, stats in ((dx, "x", M * K, sx), (dw, "w", N * K, sw)):
         value, bound = want["d" + key], want["b" + key]
         within(got[:n], value, bound + H * (value.abs() + bound) + 2.0 ** -25, "d" + key)
-        assert float((got[:n].double().view_as(value) - value).norm() / value.norm()) <= H
+        if M > 50 and N > 50:  # (many roundings in a sum, many sums)
+            assert float((got[:n].double().view_as(value) - value).norm() / value.norm()) <= H
         amax, bad, _ = mp8.read_stats(stats)
         top = torch.tensor([amax], dtype=torch.int32).view(torch.float32)
         assert bad == 0 and abs(float(top) - float(value.abs().max())) <= float(bound.max())
@@ -140,7 +144,9 @@ def momentum(mp8, w, v, g, lr, **kw):
 @pytest.mark.parametrize("batch,rows,cols", [
     (1, 40, 8192), (1, 8192, 40), (5, 30, 2100), (3, 3001, 65), (2, 100, 5000), (1, 1, 20000), (1, 129, 30001), (1, 260, 8192), (1, 1024, 1024),
     (1, 1001, 1003), (9, 500, 520), (20, 257, 389), (1, 1500, 1499), (1, 2049, 2560), (2, 2100, 4099), (1, 4100, 3700), (1, 700, 20011), (1, 20011, 700),
-    (1, 4104, 6200)])
+    (1, 4104, 6200), (61, 3571, 1), (54, 886, 1), (37, 303, 269), (3, 1631, 1170), (35, 597, 564), (4, 5039, 1281), (15, 1244, 972), (1, 15047, 2989),
+    (54, 2, 896), (21, 1, 10872), (43, 259, 283), (3, 1128, 1413), (41, 575, 712), (8, 920, 5333), (16, 1001, 1032), (1, 2956, 13518), (1, 835, 901),
+    (1, 854, 835), (13, 2732, 134), (16, 132, 2134), (1, 865, 9807), (1, 8478, 994)])
 def test_direction_of_large_tiles(mp8, batch, rows, cols):
     gen = torch.Generator(device="cuda").manual_seed(rows + cols)
     g = codes(torch.randn((batch, rows, cols), generator=gen, device="cuda"))
