@@ -192,6 +192,127 @@ struct OrthoUpdate : HalfNoneAhead {
 };
 
 // ---------------------------------------------------------------------------------------
+// Short sides: polynomial and product in one launch.  Every workgroup (a 64x64 tile of the product) makes the 64 rows of
+// P = b A + c A A that its tile needs, from all of A in LDS, rounds them to half as the pass of its own would, and multiplies them with
+// its part of X, which was requested together with A.  That is up to m / 64 times as many products as necessary, but a launch of its own
+// costs 3 to 5 us whatever it multiplies.
+// ---------------------------------------------------------------------------------------
+struct OrthoJoint {
+    const uint16_t *a, *x;
+    int64_t a_batch, x_batch;  // in halves
+    int m, m8, rows;           // of A, up to a multiple of eight, of X
+    const uint32_t *skip;
+};
+// TALL: X P, the tile's rows of X as they are; otherwise P X, a panel of X, read transposed.  LDS images as half_gemm_kernel's.  S: slabs of
+// 64 of the shorter side, so that all reads of LDS can be requested at once (with a loop of unknown length 10 us instead of 5.1 at 128x128).
+template <int S, bool TALL, class Epi>
+__global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const OrthoJoint p, const Epi epi) {
+    constexpr int A_SLAB = S * 64 * 128, S_SLAB = 64 * 128;  // per 64 columns: all of A; 64 rows of P or X
+    constexpr bool LATER = S * (A_SLAB + 2 * S_SLAB) > 160 * 1024;  // X takes A's place, and waits in registers until it is free
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * (A_SLAB + (LATER ? 1 : 2) * S_SLAB)];
+    uint8_t *const la = lds, *const lp = lds + S * A_SLAB, *const lx = LATER ? la : lp + S * S_SLAB;
+    if (p.skip != nullptr && *p.skip != 0u) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int batch = blockIdx.y, along = blockIdx.x / S, band = blockIdx.x % S;  // (S tiles along the shorter side)
+    const int tm = TALL ? along : band, tn = TALL ? band : along;
+    const uint16_t *a = p.a + batch * p.a_batch, *x = p.x + batch * p.x_batch;
+
+    auto row_slot = [](int r, int c) { return r * 128 + ((c ^ ((r >> 1) & 7)) << 4); };  // chunk c of row r, contraction along the row
+    const int r0 = threadIdx.x >> 3, c0 = threadIdx.x & 7;
+    u32x4 va[S][2 * S], vx[2 * S];  // [panel][32 rows]; see below
+#pragma unroll
+    for (int h = 0; h < S; ++h)
+#pragma unroll
+        for (int q = 0; q < 2 * S; ++q) {
+            const int r = 32 * q + r0, c = 64 * h + 8 * c0;
+            va[h][q] = u32x4{0, 0, 0, 0};
+            if (r < p.m && c < p.m8) va[h][q] = *reinterpret_cast<const u32x4 *>(a + HalfMatrix::at(r, c, 64 * (int64_t)p.m));
+        }
+#pragma unroll
+    for (int q = 0; q < 2 * S; ++q) {
+        vx[q] = u32x4{0, 0, 0, 0};
+        if constexpr (TALL) {  // panel q / 2, rows 32 (q % 2) + r0 of the tile
+            const int r = 64 * along + 32 * (q & 1) + r0, c = 64 * (q >> 1) + 8 * c0;
+            if (r < p.rows && c < p.m8) vx[q] = *reinterpret_cast<const u32x4 *>(x + HalfMatrix::at(r, c, 64 * (int64_t)p.rows));
+        } else {  // rows 32 q + r0 of the panel
+            const int r = 32 * q + r0;
+            if (r < p.rows) vx[q] = *reinterpret_cast<const u32x4 *>(x + HalfMatrix::at(r, 64 * along + 8 * c0, 64 * (int64_t)p.rows));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < S; ++h)
+#pragma unroll
+        for (int q = 0; q < 2 * S; ++q) *reinterpret_cast<u32x4 *>(la + h * A_SLAB + row_slot(32 * q + r0, c0)) = va[h][q];
+    auto put_x = [&]() {
+#pragma unroll
+        for (int q = 0; q < 2 * S; ++q) {
+            if constexpr (TALL) *reinterpret_cast<u32x4 *>(lx + (q >> 1) * S_SLAB + row_slot(32 * (q & 1) + r0, c0)) = vx[q];
+            else *reinterpret_cast<u32x4 *>(lx + (32 * q + r0) * 128 + ((c0 ^ (((r0 >> 1) & 1) << 2)) << 4)) = vx[q];
+        }
+    };
+    if constexpr (!LATER) put_x();
+    __syncthreads();
+
+    const int frow = lane & 31, fk = lane >> 5, t16 = lane & 15;
+    auto row_fragment = [&](const uint8_t *image, int slab, int sub, int m) {
+        return *reinterpret_cast<const half8 *>(image + (sub >> 2) * slab + row_slot(m + frow, 2 * (sub & 3) + fk));
+    };
+    {  // this wave's 32 rows of P, columns 32 (S wn + i) ..
+        f32x16 acc[S];
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][e] = 0.0f;
+#pragma unroll
+        for (int sub = 0; sub < 4 * S; ++sub) {
+            const half8 fa = row_fragment(la, A_SLAB, sub, 64 * band + 32 * wm);
+#pragma unroll
+            for (int i = 0; i < S; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(row_fragment(la, A_SLAB, sub, 32 * (S * wn + i)), fa, acc[i], 0, 0, 0);
+        }
+        const int r = 32 * wm + frow;
+#pragma unroll
+        for (int i = 0; i < S; ++i)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                using half4 = _Float16 __attribute__((ext_vector_type(4)));
+                const int c = 32 * (S * wn + i) + 8 * g, slab = c >> 6;
+                const half4 h = *reinterpret_cast<const half4 *>(la + slab * A_SLAB + row_slot(64 * band + r, (c & 63) >> 3) + 8 * fk);
+                half4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = (_Float16)__builtin_fmaf(kOrthoB, (float)h[e], kOrthoC * kDown * acc[i][4 * g + e]);
+                *reinterpret_cast<half4 *>(lp + slab * S_SLAB + row_slot(r, (c & 63) >> 3) + 8 * fk) = o;
+            }
+    }
+    __syncthreads();
+    if constexpr (LATER) {
+        put_x();
+        __syncthreads();
+    }
+
+    const int kt = 8 * fk + (t16 >> 2), ct = ((lane >> 4) & 1) * 2 + ((t16 & 3) >> 1);
+    const int ft = kt * 128 + ((ct ^ (((t16 >> 3) & 1) << 2)) << 4) + 8 * (t16 & 1);
+    auto panel_fragment = [&](int sub, int m) {  // columns m .. m + 31 of the panel
+        using h4 = short __attribute__((ext_vector_type(4)));
+        using lds_h4 = __attribute__((address_space(3))) h4;
+        const uint8_t *at = lx + (ft ^ ((m & 32) << 1)) + 16 * sub * 128;
+        const h4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4 *)at), hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_h4 *)(at + 512));
+        return __builtin_bit_cast(half8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    f32x16 acc[1][1];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[0][0][e] = 0.0f;
+#pragma unroll
+    for (int sub = 0; sub < 4 * S; ++sub) {
+        const half8 fa = row_fragment(TALL ? lx : lp, S_SLAB, sub, 32 * wm);
+        const half8 fb = TALL ? row_fragment(lp, S_SLAB, sub, 32 * wn) : panel_fragment(sub, 32 * wn);
+        acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb, fa, acc[0][0], 0, 0, 0);
+    }
+    const HalfPlace<Half64> at{batch, 0, tm, tn, 64 * tm + 32 * wm, 64 * tn + 32 * wn, wave, lane, lds};
+    epi(at, acc, HalfNothing{});
+}
+
+// ---------------------------------------------------------------------------------------
 // Momentum, and the squared norm of the direction (in double: neither squares of gradients around 1e-25 nor those around 1e25 leave its
 // range).  `blocks` workgroups per matrix.
 // ---------------------------------------------------------------------------------------
@@ -365,6 +486,14 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     return l;
 }
 
+// Whether polynomial and product go together: shorter sides up to 64 always, up to 256 while all workgroups run at once (two per CU, from three
+// slabs on one).  A whole call, us, apart / together: 64x64 50 / 34, 64 of 64x4096 267 / 188, 128x128 68 / 52, 128x20000 156 / 147, 256x256
+// 84 / 74, 256x4096 117 / 116; with more workgroups 64 of 128x1024 149 / 191, 8 of 192x768 96 / 108, 256x8192 143 / 170.
+bool ortho_joint(const OrthoLayout &l, int64_t batch) {
+    const int64_t across = (l.m + 63) / 64, tiles = batch * across * ((l.n + 63) / 64);
+    return across == 1 || (across <= 4 && tiles <= (across == 2 ? 512 : 256));
+}
+
 mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
     if (batch < 0 || rows < 0 || cols < 0) return MP8_ERR_INVALID_ARG;
     // 32-bit offsets within a tile, workgroups of a launch
@@ -430,16 +559,34 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     hipLaunchKernelGGL(ortho_start_kernel, dim3((unsigned)(blocks < 2048 ? blocks : 2048), (unsigned)batch), dim3(256), 0, st, start);
     if (!ok()) return MP8_ERR_HIP;
     const HalfMatrix A = HalfMatrix::panels(a, l.m, ab), P = HalfMatrix::panels(b, l.m, ab);
+    const bool joint = ortho_joint(l, batch);
     for (int k = 0; k < steps; ++k) {
         const HalfMatrix X = HalfMatrix::panels(x[k & 1], rows, xb);
         const OrthoSymmetric<false> gram{{}, nullptr, a, a_panel, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
         if (rows <= cols ? !ortho_product<false, false>(l.gram, batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, parts, arrived, gram, st)
                          : !ortho_product<true, true>(l.gram, batch, X, X, m8, m8, l.n, true, skip_if_nonzero, parts, arrived, gram, st))
             return MP8_ERR_HIP;
-        const OrthoSymmetric<true> poly{{}, a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
-        if (!ortho_product<false, false>(half_plan(batch, l.m, l.m, l.m, true, 1), batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, nullptr, nullptr, poly, st))
-            return MP8_ERR_HIP;
+        if (!joint) {
+            const OrthoSymmetric<true> poly{{}, a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+            if (!ortho_product<false, false>(half_plan(batch, l.m, l.m, l.m, true, 1), batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, nullptr, nullptr, poly, st))
+                return MP8_ERR_HIP;
+        }
         auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
+            if (joint) {
+                const OrthoJoint p{a, X.p, ab, xb, (int)l.m, (int)m8, (int)rows, skip_if_nonzero};
+                const int64_t across = (l.m + 63) / 64;
+                const dim3 grid((unsigned)(across * ((l.n + 63) / 64)), (unsigned)batch);
+                auto launch = [&](auto slabs) {
+                    constexpr int S = decltype(slabs)::value;
+                    if (rows <= cols) hipLaunchKernelGGL((ortho_joint_kernel<S, false, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
+                    else hipLaunchKernelGGL((ortho_joint_kernel<S, true, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
+                };
+                if (across == 1) launch(std::integral_constant<int, 1>{});
+                else if (across == 2) launch(std::integral_constant<int, 2>{});
+                else if (across == 3) launch(std::integral_constant<int, 3>{});
+                else launch(std::integral_constant<int, 4>{});
+                return ok();
+            }
             const HalfPlan plan = half_plan(batch, rows, cols, l.m, false, 1);
             return rows <= cols ? ortho_product<false, true>(plan, batch, P, X, rows, c8, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st)
                                 : ortho_product<false, false>(plan, batch, X, P, rows, cols, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st);

@@ -146,7 +146,9 @@ def momentum(mp8, w, v, g, lr, **kw):
     (1, 1001, 1003), (9, 500, 520), (20, 257, 389), (1, 1500, 1499), (1, 2049, 2560), (2, 2100, 4099), (1, 4100, 3700), (1, 700, 20011), (1, 20011, 700),
     (1, 4104, 6200), (61, 3571, 1), (54, 886, 1), (37, 303, 269), (3, 1631, 1170), (35, 597, 564), (4, 5039, 1281), (15, 1244, 972), (1, 15047, 2989),
     (54, 2, 896), (21, 1, 10872), (43, 259, 283), (3, 1128, 1413), (41, 575, 712), (8, 920, 5333), (16, 1001, 1032), (1, 2956, 13518), (1, 835, 901),
-    (1, 854, 835), (13, 2732, 134), (16, 132, 2134), (1, 865, 9807), (1, 8478, 994)])
+    (1, 854, 835), (13, 2732, 134), (16, 132, 2134), (1, 865, 9807), (1, 8478, 994),
+    (1, 64, 64), (70, 64, 1000), (70, 1000, 64), (1, 127, 129), (1, 129, 127), (6, 128, 700), (6, 700, 128), (9, 128, 4000), (2, 160, 1000), (2, 1000, 185),
+    (1, 192, 192), (1, 193, 255), (3, 256, 256), (1, 3000, 249), (1, 250, 9000)])
 def test_direction_of_large_tiles(mp8, batch, rows, cols):
     gen = torch.Generator(device="cuda").manual_seed(rows + cols)
     g = codes(torch.randn((batch, rows, cols), generator=gen, device="cuda"))
