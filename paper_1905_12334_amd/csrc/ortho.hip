@@ -23,28 +23,82 @@ namespace mp8 {
 constexpr float kOrthoA = 3.4445f, kOrthoB = -4.7750f, kOrthoC = 2.0315f;
 constexpr float kUp = 16384.0f, kDown = 1.0f / 16384.0f;  // the scale of A and of the polynomial
 
-// linear * x + scale * sum, as halves.
-__device__ __forceinline__ u32x4 ortho_combine(float linear, const u32x4 &x, float scale, const float (&sum)[8]) {
-    const half8 h = __builtin_bit_cast(half8, x);
-    float v[8];
+// Polynomials are operands in halves (times 2^14).  What the rounding takes from their diagonal, d, is kept in FP32 and comes back
+// with the term in a: (a + d) x + sum.  Near the end the diagonal is the largest part of every row (b A + c A^2 is near (b + c) I), and its
+// rounding was the largest of all errors: of the update of a noisy 700 x 1500 gradient 1.3e-3 of its norm, with d 0.86e-3.
+__device__ __forceinline__ float ortho_combine(float d, float x, float sum) { return __builtin_fmaf(__builtin_fmaf(kDown, d, kOrthoA), x, kDown * sum); }
+__device__ __forceinline__ float ortho_lost(float v) { return v - (float)(_Float16)v; }
+
+// d where the next iterate's epilogues want it: of the rows (one per lane and band), or (TALL) of a lane's eight columns.
+template <class T, bool TALL>
+struct OrthoDiagonal {
+    float d[TALL ? 8 : T::MT];
+};
+template <bool TALL, class T>
+__device__ __forceinline__ OrthoDiagonal<T, TALL> ortho_diagonal(const HalfPlace<T> &at, const float *diagonal, int m) {
+    OrthoDiagonal<T, TALL> in;
+    if constexpr (TALL) {
+        const int c = at.col0 + 8 * (at.lane % (T::WTN / 8));
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(linear, (float)h[e], scale * sum[e]);
-    return half_operand8(v);
+        for (int e = 0; e < 8; ++e) in.d[e] = c + e < m ? diagonal[c + e] : 0.0f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < T::MT; ++i) {
+            const int r = at.row0 + 32 * i + (at.lane & 31);
+            in.d[i] = r < m ? diagonal[r] : 0.0f;
+        }
+    }
+    return in;
+}
+// f(r, c, v, x) as in half_bands, v with the elements of d instead of a: for rows they lie behind the band's columns.
+template <int MOST_U, bool TALL, class T, class Load, class F>
+__device__ __forceinline__ void ortho_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const OrthoDiagonal<T, TALL> &in, const Load &load, const F &f) {
+    const float *rows = nullptr;
+    half_bands<MOST_U>(at, acc, load, [&](int r, int c, const float (&sum)[8], const decltype(load(0, 0)) &x) {
+        float d[8];
+        const float row = TALL ? 0.0f : rows[((r - at.row0) & 31) * kHalfBandPitch<T>];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = TALL ? in.d[TALL ? e : 0] : row;
+        f(r, c, sum, d, x);
+    }, [&](int i, float *band) {
+        if constexpr (!TALL) {
+            if (at.lane < 32) band[at.lane * kHalfBandPitch<T> + T::WTN] = in.d[i];
+            rows = band + T::WTN;
+        }
+    });
 }
 
 // A symmetric output of halves, made from its upper tiles: v = scale * acc (POLY: + linear * in[r, c]) at (r, c) and, off the diagonal's
 // tiles, at (c, r), turned round by the lanes that read the band.  Columns m .. m8 - 1 are zero.
 // With the conversions of the results' epilogues (canonical NaN, a test per element) two bands of a 128x128 tile took 5 us.
 template <bool POLY>
-struct OrthoSymmetric : HalfNoneAhead {
-    static constexpr bool kJoin = !POLY;
+struct OrthoSymmetric {
+    static constexpr bool kJoin = !POLY, k192 = true;
     const uint16_t *in;
     uint16_t *out;
     int64_t panel, batch;  // in halves
     int m;
     float linear, scale;
+    float *diagonal;  // POLY: what the halves' diagonal lacks
+    int64_t diagonal_batch;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
+    struct Ahead {
+        float d[T::MT];  // in[r, r] of this lane's rows, in a wave's part on the diagonal
+    };
+    template <class T>
+    __device__ __forceinline__ Ahead<T> ahead(const HalfPlace<T> &at) const {
+        Ahead<T> a{};
+        if (POLY && at.row0 == at.col0) {
+#pragma unroll
+            for (int i = 0; i < T::MT; ++i) {
+                const int r = at.row0 + 32 * i + (at.lane & 31);
+                if (r < m) a.d[i] = half_bits_to_f32(in[at.batch * batch + HalfMatrix::at(r, r, panel)]);
+            }
+        }
+        return a;
+    }
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const Ahead<T> &ahead) const {
         const uint16_t *x = in + at.batch * batch;
         uint16_t *o = out + at.batch * batch;
         const bool mirror = at.tm != at.tn;
@@ -53,16 +107,18 @@ struct OrthoSymmetric : HalfNoneAhead {
             if (POLY && r < m && c < m) xw = *reinterpret_cast<const u32x4 *>(x + HalfMatrix::at(r, c, panel));
             return xw;
         };
-        auto value = [&](const u32x4 &xw, const float (&sum)[8]) {
-            if constexpr (POLY) return ortho_combine(linear, xw, scale, sum);
-            float v[8];
+        auto value = [&](const u32x4 &xw, float (&v)[8]) {
+            const half8 h = __builtin_bit_cast(half8, xw);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = scale * sum[e];
-            return half_operand8(v);
+            for (int e = 0; e < 8; ++e) v[e] = POLY ? __builtin_fmaf(linear, (float)h[e], scale * v[e]) : scale * v[e];
         };
         half_bands(at, acc, load, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
             if (r >= m || c >= m) return;
-            u32x4 w = value(xw, sum);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = sum[e];
+            value(xw, v);
+            u32x4 w = half_operand8(v);
             if (m - c < 8) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -70,6 +126,11 @@ struct OrthoSymmetric : HalfNoneAhead {
             }
             *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(r, c, panel)) = w;
         }, [&](int i, const float *band) {
+            if (POLY && at.row0 == at.col0) {
+                const int k = at.lane & 31, r = at.row0 + 32 * i + k;
+                if (at.lane < 32 && r < m)
+                    diagonal[at.batch * diagonal_batch + r] = ortho_lost(__builtin_fmaf(linear, ahead.d[i], scale * band[k * kHalfBandPitch<T> + 32 * i + k]));
+            }
             if (!mirror) return;
             // four lanes per row of the turned band: its rows are the band's columns, its columns rows of the tile, all of which exist
             // (a tile below the diagonal's ends at a tile border)
@@ -83,10 +144,11 @@ struct OrthoSymmetric : HalfNoneAhead {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int n = n0 + 16 * u, c = at.col0 + n;
-                    float sum[8];
+                    float v[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] = band[(k + e) * kHalfBandPitch<T> + n];
-                    if (c < m) *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(c, r, panel)) = value(xw[u], sum);
+                    for (int e = 0; e < 8; ++e) v[e] = band[(k + e) * kHalfBandPitch<T> + n];
+                    value(xw[u], v);
+                    if (c < m) *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(c, r, panel)) = half_operand8(v);
                 }
             }
         });
@@ -94,37 +156,57 @@ struct OrthoSymmetric : HalfNoneAhead {
 };
 
 // The next iterate, a X + scale * acc, as halves.  Columns up to the next multiple of eight are stored (they are zero).
-struct OrthoNext : HalfNoneAhead {
+template <bool TALL>
+struct OrthoNext {
+    static constexpr bool kJoin = false, k192 = true;
     const uint16_t *x;
     uint16_t *out;
     int64_t panel, batch;  // in halves
     int rows, cols;
+    const float *diagonal;
+    int64_t diagonal_batch;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
+    __device__ __forceinline__ OrthoDiagonal<T, TALL> ahead(const HalfPlace<T> &at) const {
+        return ortho_diagonal<TALL>(at, diagonal + at.batch * diagonal_batch, TALL ? cols : rows);
+    }
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const OrthoDiagonal<T, TALL> &ahead) const {
         const int64_t base = at.batch * batch;
-        half_bands(at, acc, [&](int r, int c) {
+        ortho_bands<4, TALL>(at, acc, ahead, [&](int r, int c) {
             u32x4 xw = {0, 0, 0, 0};
             if (r < rows && c < cols) xw = *reinterpret_cast<const u32x4 *>(x + base + HalfMatrix::at(r, c, panel));
             return xw;
-        }, [&](int r, int c, const float (&sum)[8], const u32x4 &xw) {
+        }, [&](int r, int c, const float (&sum)[8], const float (&d)[8], const u32x4 &xw) {
             if (r >= rows || c >= cols) return;
-            *reinterpret_cast<u32x4 *>(out + base + HalfMatrix::at(r, c, panel)) = ortho_combine(kOrthoA, xw, kDown, sum);
-        }, [](int, float *) {});
+            const half8 h = __builtin_bit_cast(half8, xw);
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = ortho_combine(d[e], (float)h[e], sum[e]);
+            *reinterpret_cast<u32x4 *>(out + base + HalfMatrix::at(r, c, panel)) = half_operand8(v);
+        });
     }
 };
 
 // The last iterate goes straight into the weights: w' = w - lr (X + wd w), rounded to half, and its 8-bit copy.
-struct OrthoUpdate : HalfNoneAhead {
+template <bool TALL>
+struct OrthoUpdate {
+    static constexpr bool kJoin = false, k192 = true;
     const uint16_t *x;
     int64_t panel, batch;
     int rows, cols;
+    const float *diagonal;
+    int64_t diagonal_batch;
     float inv_s, neg_lr, wd;
     uint16_t *w16;
     uint8_t *w8;
     int sr;
     uint64_t seed, offset;
     template <class T>
-    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
+    __device__ __forceinline__ OrthoDiagonal<T, TALL> ahead(const HalfPlace<T> &at) const {
+        return ortho_diagonal<TALL>(at, diagonal + at.batch * diagonal_batch, TALL ? cols : rows);
+    }
+    template <class T>
+    __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const OrthoDiagonal<T, TALL> &ahead) const {
         const Philox rng(seed, offset);
         const bool whole = (cols & 7) == 0;
         const int64_t first = (int64_t)at.batch * rows * cols;
@@ -132,7 +214,7 @@ struct OrthoUpdate : HalfNoneAhead {
             u32x4 x, w;
         };
         // (four copies of this code per band are too much for the compiler where there are three or four bands)
-        half_bands<(T::BM > 128 ? 1 : 4)>(at, acc, [&](int r, int c) {
+        ortho_bands<(T::BM > 128 ? 1 : 4), TALL>(at, acc, ahead, [&](int r, int c) {
             Eight in{};
             if (r >= rows || c >= cols) return in;
             in.x = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + HalfMatrix::at(r, c, panel));
@@ -145,7 +227,7 @@ struct OrthoUpdate : HalfNoneAhead {
                     if (c + e < cols) in.w[e >> 1] |= (uint32_t)w16[i0 + e] << (16 * (e & 1));
             }
             return in;
-        }, [&](int r, int c, const float (&sum)[8], const Eight &in) {
+        }, [&](int r, int c, const float (&sum)[8], const float (&diag)[8], const Eight &in) {
             if (r >= rows || c >= cols) return;
             const int64_t i0 = first + (int64_t)r * cols + c;
             const int n = cols - c < 8 ? cols - c : 8;
@@ -166,7 +248,7 @@ struct OrthoUpdate : HalfNoneAhead {
                 uint32_t hw[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float d = __builtin_fmaf(kOrthoA, half_bits_to_f32(xw[q] >> (16 * e)), kDown * sum[2 * q + e]) * inv_s;
+                    const float d = ortho_combine(diag[2 * q + e], half_bits_to_f32(xw[q] >> (16 * e)), sum[2 * q + e]) * inv_s;
                     const float f = half_bits_to_f32(ww[q] >> (16 * e));
                     float wn = __builtin_fmaf(neg_lr, __builtin_fmaf(wd, f, d), f);
                     asm volatile("" : "+v"(wn));  // (two roundings: see update_four)
@@ -187,7 +269,7 @@ struct OrthoUpdate : HalfNoneAhead {
                         if (w8 != nullptr) w8[i0 + e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
                     }
             }
-        }, [](int, float *) {});
+        });
     }
 };
 
@@ -209,7 +291,9 @@ template <int S, bool TALL, class Epi>
 __global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const OrthoJoint p, const Epi epi) {
     constexpr int A_SLAB = S * 64 * 128, S_SLAB = 64 * 128;  // per 64 columns: all of A; 64 rows of P or X
     constexpr bool LATER = S * (A_SLAB + 2 * S_SLAB) > 160 * 1024;  // X takes A's place, and waits in registers until it is free
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[S * (A_SLAB + (LATER ? 1 : 2) * S_SLAB)];
+    constexpr int OPERANDS = S * (A_SLAB + (LATER ? 1 : 2) * S_SLAB);
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[OPERANDS + (LATER ? 0 : 256)];
+    float *const diagonal = reinterpret_cast<float *>(lds + (LATER ? A_SLAB * S / 2 : OPERANDS));  // of the band (LATER: in A's place too)
     uint8_t *const la = lds, *const lp = lds + S * A_SLAB, *const lx = LATER ? la : lp + S * S_SLAB;
     if (p.skip != nullptr && *p.skip != 0u) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
@@ -257,6 +341,9 @@ __global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const O
     auto row_fragment = [&](const uint8_t *image, int slab, int sub, int m) {
         return *reinterpret_cast<const half8 *>(image + (sub >> 2) * slab + row_slot(m + frow, 2 * (sub & 3) + fk));
     };
+    const int own = 32 * wm + frow;  // row of the band
+    float own_diagonal = 0.0f;
+    bool has_diagonal = false;
     {  // this wave's 32 rows of P, columns 32 (S wn + i) ..
         f32x16 acc[S];
 #pragma unroll
@@ -270,21 +357,35 @@ __global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const O
             for (int i = 0; i < S; ++i)
                 acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(row_fragment(la, A_SLAB, sub, 32 * (S * wn + i)), fa, acc[i], 0, 0, 0);
         }
-        const int r = 32 * wm + frow;
 #pragma unroll
-        for (int i = 0; i < S; ++i)
+        for (int i = 0; i < S; ++i) {
+            using half4 = _Float16 __attribute__((ext_vector_type(4)));
+            const int block = S * wn + i;
+            float v[4][4];
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                using half4 = _Float16 __attribute__((ext_vector_type(4)));
-                const int c = 32 * (S * wn + i) + 8 * g, slab = c >> 6;
-                const half4 h = *reinterpret_cast<const half4 *>(la + slab * A_SLAB + row_slot(64 * band + r, (c & 63) >> 3) + 8 * fk);
+                const half4 h = *reinterpret_cast<const half4 *>(la + (block >> 1) * A_SLAB + row_slot(64 * band + own, 4 * (block & 1) + g) + 8 * fk);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[g][e] = __builtin_fmaf(kOrthoB, (float)h[e], kOrthoC * kDown * acc[i][4 * g + e]);
+            }
+            if (block == 2 * band + wm) {  // (of the columns 8 g + 4 fk + e, frow)
+                has_diagonal = ((frow >> 2) & 1) == fk;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) own_diagonal = 8 * g + 4 * fk + e == frow ? v[g][e] : own_diagonal;
+            }
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
                 half4 o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = (_Float16)__builtin_fmaf(kOrthoB, (float)h[e], kOrthoC * kDown * acc[i][4 * g + e]);
-                *reinterpret_cast<half4 *>(lp + slab * S_SLAB + row_slot(r, (c & 63) >> 3) + 8 * fk) = o;
+                for (int e = 0; e < 4; ++e) o[e] = (_Float16)v[g][e];
+                *reinterpret_cast<half4 *>(lp + (block >> 1) * S_SLAB + row_slot(own, 4 * (block & 1) + g) + 8 * fk) = o;
             }
+        }
     }
     __syncthreads();
+    if (has_diagonal) diagonal[own] = ortho_lost(own_diagonal);
     if constexpr (LATER) {
         put_x();
         __syncthreads();
@@ -309,7 +410,9 @@ __global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const O
         acc[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fb, fa, acc[0][0], 0, 0, 0);
     }
     const HalfPlace<Half64> at{batch, 0, tm, tn, 64 * tm + 32 * wm, 64 * tn + 32 * wn, wave, lane, lds};
-    epi(at, acc, HalfNothing{});
+    HalfPlace<Half64> in_band = at;  // (the diagonal counts from the band's first row or column)
+    (TALL ? in_band.col0 : in_band.row0) -= 64 * band;
+    epi(at, acc, ortho_diagonal<TALL>(in_band, diagonal, 64));
 }
 
 // ---------------------------------------------------------------------------------------
@@ -456,7 +559,7 @@ struct OrthoLayout {
     int blocks;             // workgroups of the momentum pass per matrix
     HalfPlan gram;
     int64_t words;          // tiles of the Gram matrices
-    size_t squares, x0, x1, a, b, parts, arrived, total;
+    size_t squares, x0, x1, a, b, diagonal, parts, arrived, total;
 };
 OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     OrthoLayout l{};
@@ -480,6 +583,7 @@ OrthoLayout ortho_layout(int64_t batch, int64_t rows, int64_t cols) {
     l.x1 = take(2 * batch * l.x_batch);
     l.a = take(2 * batch * l.a_batch);
     l.b = take(2 * batch * l.a_batch);
+    l.diagonal = take(4 * batch * up(l.m, 64));
     l.parts = take(4 * l.words * l.gram.splits * l.gram.tile * l.gram.tile);
     l.arrived = take(4 * l.words);
     l.total = at;
@@ -544,7 +648,7 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     hipStream_t st = (hipStream_t)stream;
     double *squares = (double *)(ws + l.squares);
     uint16_t *x[2] = {(uint16_t *)(ws + l.x0), (uint16_t *)(ws + l.x1)}, *a = (uint16_t *)(ws + l.a), *b = (uint16_t *)(ws + l.b);
-    float *parts = (float *)(ws + l.parts);
+    float *parts = (float *)(ws + l.parts), *diagonal = (float *)(ws + l.diagonal);
     uint32_t *arrived = (uint32_t *)(ws + l.arrived);
     const double s = std::exp2(std::nearbyint(0.5 * std::log2((double)l.n)));
     const auto ok = [] { return hipGetLastError() == hipSuccess; };
@@ -552,7 +656,7 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const OrthoMomentum mom{velocity, g8, rows * cols, inv_loss_scale, momentum, nesterov, l.blocks, skip_if_nonzero, squares, stats, arrived, (int)l.words};
     hipLaunchKernelGGL(ortho_momentum_kernel, dim3((unsigned)l.blocks, (unsigned)batch), dim3(256), 0, st, mom);
     if (!ok()) return MP8_ERR_HIP;
-    const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = l.x_batch, ab = l.a_batch, x_panel = 64 * rows, a_panel = 64 * l.m;
+    const int64_t c8 = up(cols, 8), m8 = up(l.m, 8), xb = l.x_batch, ab = l.a_batch, x_panel = 64 * rows, a_panel = 64 * l.m, db = up(l.m, 64);
     const OrthoStart start{velocity, g8, (int)rows, (int)cols, inv_loss_scale, momentum, nesterov, l.blocks, squares, skip_if_nonzero, s, x[0], xb,
                            make_fastdiv((uint32_t)(c8 / 8))};
     const int64_t blocks = up(rows * (c8 / 8), 256) / 256;
@@ -562,39 +666,39 @@ extern "C" mp8_status mp8_orthogonal_momentum_fp16_sr(int64_t batch, int64_t row
     const bool joint = ortho_joint(l, batch);
     for (int k = 0; k < steps; ++k) {
         const HalfMatrix X = HalfMatrix::panels(x[k & 1], rows, xb);
-        const OrthoSymmetric<false> gram{{}, nullptr, a, a_panel, ab, (int)l.m, 0.0f, (float)(kUp / (s * s))};
+        const OrthoSymmetric<false> gram{nullptr, a, a_panel, ab, (int)l.m, 0.0f, (float)(kUp / (s * s)), nullptr, 0};
         if (rows <= cols ? !ortho_product<false, false>(l.gram, batch, X, X, l.m, l.m, l.n, true, skip_if_nonzero, parts, arrived, gram, st)
                          : !ortho_product<true, true>(l.gram, batch, X, X, m8, m8, l.n, true, skip_if_nonzero, parts, arrived, gram, st))
             return MP8_ERR_HIP;
         if (!joint) {
-            const OrthoSymmetric<true> poly{{}, a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown};
+            const OrthoSymmetric<true> poly{a, b, a_panel, ab, (int)l.m, kOrthoB, kOrthoC * kDown, diagonal, db};
             if (!ortho_product<false, false>(half_plan(batch, l.m, l.m, l.m, true, 1), batch, A, A, l.m, l.m, l.m, true, skip_if_nonzero, nullptr, nullptr, poly, st))
                 return MP8_ERR_HIP;
         }
-        auto second = [&](auto epi) {  // (the polynomial is symmetric: its rows are its columns)
+        // X' or the weights, made by `epi` (the polynomial is symmetric: its rows are its columns)
+        auto second = [&](auto tall, auto epi) {
+            constexpr bool TALL = decltype(tall)::value;
             if (joint) {
                 const OrthoJoint p{a, X.p, ab, xb, (int)l.m, (int)m8, (int)rows, skip_if_nonzero};
                 const int64_t across = (l.m + 63) / 64;
                 const dim3 grid((unsigned)(across * ((l.n + 63) / 64)), (unsigned)batch);
-                auto launch = [&](auto slabs) {
-                    constexpr int S = decltype(slabs)::value;
-                    if (rows <= cols) hipLaunchKernelGGL((ortho_joint_kernel<S, false, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
-                    else hipLaunchKernelGGL((ortho_joint_kernel<S, true, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
-                };
-                if (across == 1) launch(std::integral_constant<int, 1>{});
-                else if (across == 2) launch(std::integral_constant<int, 2>{});
-                else if (across == 3) launch(std::integral_constant<int, 3>{});
-                else launch(std::integral_constant<int, 4>{});
+                if (across == 1) hipLaunchKernelGGL((ortho_joint_kernel<1, TALL, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
+                else if (across == 2) hipLaunchKernelGGL((ortho_joint_kernel<2, TALL, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
+                else if (across == 3) hipLaunchKernelGGL((ortho_joint_kernel<3, TALL, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
+                else hipLaunchKernelGGL((ortho_joint_kernel<4, TALL, decltype(epi)>), grid, dim3(256), 0, st, p, epi);
                 return ok();
             }
             const HalfPlan plan = half_plan(batch, rows, cols, l.m, false, 1);
-            return rows <= cols ? ortho_product<false, true>(plan, batch, P, X, rows, c8, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st)
-                                : ortho_product<false, false>(plan, batch, X, P, rows, cols, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st);
+            if constexpr (TALL) return ortho_product<false, false>(plan, batch, X, P, rows, cols, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st);
+            else return ortho_product<false, true>(plan, batch, P, X, rows, c8, l.m, false, skip_if_nonzero, nullptr, nullptr, epi, st);
         };
-        const bool last = k + 1 == steps;
-        if (!last && !second(OrthoNext{{}, X.p, x[(k + 1) & 1], x_panel, xb, (int)rows, (int)cols})) return MP8_ERR_HIP;
-        if (last && !second(OrthoUpdate{{}, X.p, x_panel, xb, (int)rows, (int)cols, (float)(1.0 / s), -lr, weight_decay, w16, w8_out, round == MP8_SR, seed, offset}))
-            return MP8_ERR_HIP;
+        auto advance = [&](auto tall) {
+            constexpr bool TALL = decltype(tall)::value;
+            if (k + 1 < steps) return second(tall, OrthoNext<TALL>{X.p, x[(k + 1) & 1], x_panel, xb, (int)rows, (int)cols, diagonal, db});
+            return second(tall, OrthoUpdate<TALL>{X.p, x_panel, xb, (int)rows, (int)cols, diagonal, db, (float)(1.0 / s), -lr, weight_decay, w16, w8_out,
+                                                  round == MP8_SR, seed, offset});
+        };
+        if (!(rows > cols ? advance(std::true_type{}) : advance(std::false_type{}))) return MP8_ERR_HIP;
     }
     return MP8_OK;
 }
