@@ -425,8 +425,9 @@ mp8_status mp8_wgrad_adam_fp16_sr(int64_t M, int64_t N, int64_t K, const uint8_t
  *              element index).  What is not asked for is not computed; one at least is.
  *   dx_stats, dw_stats   nullable: of the 8-bit codes, or of the halves where only those are asked for
  *   workspace  device scratch, 16-byte aligned, mp8_softmax_xent_{fwd,bwd}_workspace_bytes(M, N, K, ldw) bytes; contents
- *              undefined afterwards.  It grows with M * N / 16 bytes (forward) and is bounded in N backward, where the vocabulary is
- *              taken in pieces.
+ *              undefined afterwards.  Forward it grows with M * N / 8 bytes (large calls M * N / 32); backward it is bounded in N: the
+ *              vocabulary is taken in pieces.
+ * Outputs overlap neither inputs nor each other.
  * Precision: logits, the softmax's sums and the gradients' sums are FP32 (the products' operands halves); e is rounded to half, times a power of two
  * that the largest token weight sets, before it is multiplied by w and x: eleven bits, which weights of less than 2^-14 of the
  * largest lose one by one.  The results are the same from run to run.
@@ -459,7 +460,7 @@ size_t mp8_softmax_xent_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int
  *              counts there while its later launches still read the flag
  * Other arguments as for mp8_sgd_momentum_fp16_sr.  A gradient code that is Inf or NaN makes its whole matrix NaN (unless the step is
  * skipped).  Precision: the velocity is FP32 as there; the products take half operands and add up in FP32, X is off by some 1e-3 of its
- * root mean square (1e-2 where a few directions hold nearly all of u).  Results are the same from run to run.
+ * root mean square (0.7e-3 to 1.2e-3 for noise, 2e-3 with a few strong directions, 1e-2 where those hold nearly all of u).  Results are the same from run to run.
  * rows, cols <= 2^20, batch <= 65535 and batch * rows / 64 * cols / 64 <= 2^23, rounded up (MP8_ERR_UNSUPPORTED beyond).  A zero
  * dimension is valid and does nothing.
  */

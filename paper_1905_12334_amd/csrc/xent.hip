@@ -363,9 +363,7 @@ __global__ __launch_bounds__(1024) void xent_factor_kernel(const int64_t *__rest
         m = sh[0];
 #pragma unroll
         for (int k = 1; k < 16; ++k) m = __builtin_fmaxf(m, sh[k]);
-        // m < 2^e; clamped so that 2^-e is a normal number
-        e = m > 0.0f ? ilogbf(m) + 1 : 0;
-        e = e < -120 ? -120 : e > 120 ? 120 : e;
+        e = m > 0.0f ? ilogbf(m) + 1 : 0;  // m < 2^e
     }
 #pragma unroll 4
     for (int r = threadIdx.x; r < M; r += 1024)

@@ -33,7 +33,8 @@ def bytes_of(n):
 
 # ------------------------------------------------------------------ softmax cross entropy
 def truth(x, w, t, scale):
-    """Results in 64 bits and the elementwise bounds."""
+    """Results in 64 bits and the elementwise bounds; scale: of all tokens, or of each."""
+    scale = torch.as_tensor(scale, dtype=torch.float64, device="cuda").expand(x.shape[0])
     (M, K), N = x.shape, w.shape[0]
     live = (t >= 0) & (t < N)
     at, rows = torch.where(live, t, 0), torch.arange(M, device="cuda")
@@ -48,10 +49,10 @@ def truth(x, w, t, scale):
     del others
     e = torch.exp(z - lse[:, None])
     e[rows[live], t[live]] = torch.expm1(-loss[live])
-    e = torch.where(live[:, None], e, 0.0) * scale
+    e = torch.where(live[:, None], e, 0.0) * scale[:, None]
     dlse = r + 4 * U * lse.abs()  # (of tokens without a target too)
     r = torch.where(live, r, 0.0)
-    de = (H + r + 8 * U)[:, None] * e.abs() + torch.where(live, 2.0 ** -39 * scale, 0.0)[:, None]
+    de = (H + r + 8 * U)[:, None] * e.abs() + torch.where(live, 2.0 ** -39 * scale[live].abs().max(), 0.0)[:, None]
     dx, dw = e @ w, e.t() @ x
     bx, bw = de @ w.abs() + N * U * (e.abs() @ w.abs()), de.t() @ x.abs() + M * U * (e.abs().t() @ x.abs())
     return dict(loss=loss, lse=lse, r=r, dlse=dlse, dx=dx, dw=dw, bx=bx, bw=bw, live=live)
@@ -115,6 +116,25 @@ def test_cross_entropy_of_large_tiles(mp8, M, N, K):
         only = torch.empty(M * K, dtype=torch.uint8, device="cuda")
         mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dx8=only, workspace=ws, **kw)
         assert torch.equal(only, cx[:M * K])
+
+
+@pytest.mark.parametrize("size", [1e-42, 1e-37, 1e37, 3e38])
+def test_token_weights_to_the_ends_of_fp32(mp8, size):
+    M, N, K = 200, 300, 64
+    x, w, t = inputs(5, M, N, K)
+    weight = torch.full((M,), size, device="cuda")
+    weight[::3] *= 0.25
+    # (what FP32 makes of the weights; the scale's FP32 rounding is one of the 8 U in the bound)
+    scale = torch.tensor(min(16 / size, 2.0 ** 126), dtype=torch.float32).item()
+    want = truth(x.double(), w.double(), t, (weight.double() * scale))
+    loss, lse = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    mp8.softmax_xent_fwd_fp16(M, N, K, x, w, t, loss, lse, workspace=bytes_of(mp8.softmax_xent_fwd_workspace_bytes(M, N, K)))
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dloss=weight, dx16=dx, dw16=dw, scale=scale,
+                              workspace=bytes_of(mp8.softmax_xent_bwd_workspace_bytes(M, N, K)))
+    for got, key in ((dx, "x"), (dw, "w")):
+        value, bound = want["d" + key], want["b" + key]
+        within(got, value, bound + H * (value.abs() + bound) + 2.0 ** -25, "d" + key)
 
 
 # ------------------------------------------------------------------ orthogonalised momentum
