@@ -121,10 +121,10 @@ struct HalfPlace {
 //     takes the place of the current one, then the current stage is multiplied; the other workgroup fills what is left
 //   kByIndex (few tiles, long contractions): the same, but each wave multiplies the whole tile over one of the four sub-steps, so that no
 //     fragment is read from LDS twice, and the waves' sums are added up at the end; a ring of eight stages
-// Gaussian operands, contraction 4096, TFLOP/s: 4096 x 4096 in 256x256 tiles 1090, in 128x128 tiles 1015 (with the other schedule 915), in
-// 64x64 tiles 570.  What bounds them: the 256x256 tile the power such data draws (all ones: 1390) and the clock it leaves
-// (1.85 GHz, 59 % of the cycles with a matrix instruction; loads that always hit, 1550), the small ones what a CU gets from L2 (14 TB/s in
-// all).
+// Gaussian operands: 8192 x 2048 over 32768 in 256x256 tiles 838 us = 1310 TFLOP/s (a library product of these sizes 1072 us; bounded by the
+// power that such data draws and the clock it leaves, below 2 GHz), 6007 x 1000 over 37003 in 256x256 tiles 418 us = 1060, in 128x128 tiles
+// 536 us = 830 (the other schedule is 10 % slower there).  Small tiles are bounded by what a CU gets from L2 (14 TB/s in all: 0.6 us per
+// stage of 256 tiles of 128x128).
 // Slab images:
 //   row-major: row r is 128 bytes, its 16-byte chunk c sits in slot c ^ ((r >> 1) & 7)
 //   contraction-major: panels of 64 tile rows; 64 contraction rows of 128 bytes, chunk c of contraction row k in slot
