@@ -230,6 +230,90 @@ def test_two_momentum_calls_at_once_on_two_streams(mp8):
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+# ------------------------------------------------------------------ large offsets, shared workspaces
+def test_cross_entropy_beyond_2_to_the_31_elements(mp8):
+    M, N, K = 1 << 22, 67, 520
+    x, w, t = inputs(3, M, N, K)
+    assert x.numel() > 1 << 31
+    loss, lse = torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    mp8.softmax_xent_fwd_fp16(M, N, K, x, w, t, loss, lse, workspace=torch.empty(mp8.softmax_xent_fwd_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda"))
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    scale = 256.0 / M
+    mp8.softmax_xent_bwd_fp16(M, N, K, x, w, t, loss, lse, dx16=dx, dw16=dw, scale=scale,
+                              workspace=torch.empty(mp8.softmax_xent_bwd_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda"))
+    dw_want, bw = torch.zeros((N, K), dtype=torch.float64, device="cuda"), torch.zeros((N, K), dtype=torch.float64, device="cuda")
+    part = 1 << 19
+    for i in range(0, M, part):
+        rows = slice(i, i + part)
+        want = truth(x[rows].double(), w.double(), t[rows], scale)
+        within(loss[rows], want["loss"], want["loss"] * (want["r"] + 4 * U) + 1e-44, "loss")
+        within(dx[rows], want["dx"], want["bx"] + H * (want["dx"].abs() + want["bx"]) + 2.0 ** -25, "dx")
+        dw_want += want["dw"]
+        bw += want["bw"]
+    # (additions of the parts: M U of all terms covers them, their own bound has part U)
+    within(dw, dw_want, bw * (M // part) + H * (dw_want.abs() + bw) + 2.0 ** -25, "dw")
+    assert float((dw.double() - dw_want).norm() / dw_want.norm()) <= H
+
+
+def test_momentum_beyond_2_to_the_31_elements(mp8):
+    batch, rows, cols = 65535, 64, 520
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    few = codes(torch.randn((101, rows, cols), generator=gen, device="cuda"))
+    g = torch.empty((batch, rows, cols), dtype=torch.uint8, device="cuda")
+    for i in range(0, batch, 101):
+        g[i:i + 101] = few[:min(101, batch - i)]
+    assert g.numel() > 1 << 31
+    v = torch.zeros(g.shape, device="cuda")
+    w = torch.zeros(g.shape, dtype=torch.float16, device="cuda")
+    ws = torch.empty(mp8.orthogonal_momentum_workspace_bytes(batch, rows, cols), dtype=torch.uint8, device="cuda")
+    mp8.orthogonal_momentum_fp16_sr(w, v, g, -1.0, 1.0, 0.9, nesterov=False, round=mp8.RNE, workspace=ws)
+    for i in range(0, batch, 101):  # the same matrix, the same direction, wherever it lies
+        n = min(101, batch - i)
+        assert torch.equal(w[i:i + n], w[:n]) and torch.equal(v[i:i + n], v[:n])
+    for i in (0, 100):
+        u = values(few[i])
+        exact, model = iterate(u, 5, False), iterate(u, 5, True)
+        assert float((w[i].double() - exact).norm()) <= float(2 * (model - exact).norm() + H * exact.norm())
+
+
+def test_captured_graphs_that_share_a_workspace(mp8):
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    shapes = [(1, 128, 6000), (2, 200, 300), (1, 40, 9000)]  # (sliced products, whose counters lie in the workspace, and others)
+    M, N, K = 300, 2000, 200
+    x, t_w, t = inputs(2, M, N, K)
+    need = [mp8.orthogonal_momentum_workspace_bytes(*s) for s in shapes] + [mp8.softmax_xent_fwd_workspace_bytes(M, N, K), mp8.softmax_xent_bwd_workspace_bytes(M, N, K)]
+    ws = bytes_of(max(need))
+    data = [(codes(torch.randn(s, generator=gen, device="cuda")), torch.zeros(s, dtype=torch.float16, device="cuda"), torch.zeros(s, device="cuda")) for s in shapes]
+    out = [torch.empty(M, device="cuda"), torch.empty(M, device="cuda"), torch.empty_like(x), torch.empty_like(t_w)]
+
+    def update(g, w, v):
+        mp8.orthogonal_momentum_fp16_sr(w, v, g, 0.1, 1.0, 0.9, seed=2, offset=3, workspace=ws)
+
+    def loss(a, b, dx, dw):
+        mp8.softmax_xent_fwd_fp16(M, N, K, x, t_w, t, a, b, workspace=ws)
+        mp8.softmax_xent_bwd_fp16(M, N, K, x, t_w, t, a, b, dx16=dx, dw16=dw, workspace=ws)
+    eager = [(g, w.clone(), v.clone()) for g, w, v in data]
+    eager_out = [a.clone() for a in out]
+    graphs = []
+    for call, args in [(update, d) for d in data] + [(loss, out)]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(*args)
+        graphs.append(graph)
+    for k in range(4):
+        for j in ((0, 1, 2, 3), (3, 2, 1, 0), (1, 3, 0, 2), (2, 0, 3, 1))[k]:
+            graphs[j].replay()
+        torch.cuda.synchronize()
+        for d in eager:
+            update(*d)
+        loss(*eager_out)
+        torch.cuda.synchronize()
+        for a, b in zip(data, eager):
+            assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2])
+        for a, b in zip(out, eager_out):
+            assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ together
 class Step:
     """A training step: an 8-bit layer, ReLU on the codes, a last layer in FP16 with the cross entropy, the layer's weights by
