@@ -384,12 +384,14 @@ __global__ __launch_bounds__(256, S > 2 ? 1 : 2) void ortho_joint_kernel(const O
             }
         }
     }
-    __syncthreads();
-    if (has_diagonal) diagonal[own] = ortho_lost(own_diagonal);
     if constexpr (LATER) {
+        __syncthreads();  // (A has been read)
+        if (has_diagonal) diagonal[own] = ortho_lost(own_diagonal);
         put_x();
-        __syncthreads();
+    } else {
+        if (has_diagonal) diagonal[own] = ortho_lost(own_diagonal);
     }
+    __syncthreads();  // (X, P and its diagonal are complete)
 
     const int kt = 8 * fk + (t16 >> 2), ct = ((lane >> 4) & 1) * 2 + ((t16 & 3) >> 1);
     const int ft = kt * 128 + ((ct ^ (((t16 >> 3) & 1) << 2)) << 4) + 8 * (t16 & 1);
