@@ -423,19 +423,19 @@ __global__ __launch_bounds__(256, T::MINBLOCKS) void half_gemm_kernel(const Half
                     for (int g = 0; g < 4; ++g)
                         store_through(parts + (int64_t)tile.split * PART + ((i * NT + j) * 4 + g) * 64,
                                       f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
-            // Stores and loads of agent scope go past the XCDs' L2 caches, and a store that has been waited for has arrived: no cache has to
-            // be written back or emptied, as an acquiring and releasing counter would have it (4 us of 7 for 128 x 128 x 1152).
+            // The parts go past the XCDs' L2 caches, so that the counter's release has little to write back (with an acquire in every
+            // workgroup, not only the last, 128 x 128 x 1152 took 4 us longer).
             wait_vm_lds<0>();
             __syncthreads();
             uint32_t *last = reinterpret_cast<uint32_t *>(lds);
             if (threadIdx.x == 0) {
-                const uint32_t before = __hip_atomic_fetch_add(p.arrived + place, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                const uint32_t before = __hip_atomic_fetch_add(p.arrived + place, 1u, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
                 *last = before + 1u == (uint32_t)p.splits ? 1u : 0u;
                 if (*last) __hip_atomic_store(p.arrived + place, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
             __syncthreads();
             if (*last == 0u) return;
-            asm volatile("" ::: "memory");
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -547,6 +547,7 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
     }
 }
 struct HalfNothing {};
+
 template <class T, class F>
 __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f) {
     half_bands(at, acc, [](int, int) { return HalfNothing{}; }, [&](int r, int c, const float (&v)[8], HalfNothing) { f(r, c, v); }, [](int, float *) {});
@@ -627,9 +628,10 @@ static inline HalfPlan half_plan(int64_t batch, int64_t rows, int64_t cols, int6
         const int64_t tiles = batch * (symmetric ? tm * (tm + 1) / 2 : tm * tn), steps = (kc + 63) / 64;
         if (tiles > (int64_t)1 << 23) continue;
         for (int s = 1; s <= most_splits && s <= steps; s = s < 8 ? s + 1 : s + s / 4) {
-            // slices of one more pass: 4 bytes out and in again per element and slice, at 4 TB/s; joined: a tile's out
-            // and in of one CU (measured on Gram products: 128 x 128 x 1152 in 6 slices 7.0 us, unsplit 9.3; 1024 x 1024 x 4096 14.2 and 16.4)
-            const double more = s == 1 ? 0.0 : joined ? 1.5 + 4.0e-6 * (double)(tile * tile) * s * 4.0 + 1.0e-6 * (double)(tiles * tile * tile) * s
+            // slices of one more pass: 4 bytes out and in again per element and slice, at 4 TB/s; joined: a tile's out and in of one CU, and
+            // every workgroup's release of its L2 (measured on Gram products: 128 x 128 x 1152 in 6 slices 7.4 us, unsplit 9.3;
+            // 1024 x 1024 x 4096 in 3 slices of 136 tiles 20.4, unsplit 16.4)
+            const double more = s == 1 ? 0.0 : joined ? 2.0 + 1.6e-5 * (double)(tile * tile) * s + 1.0e-6 * (double)(tiles * tile * tile) * s + 0.014 * (double)(tiles * s)
                                                       : 2.0e-6 * (double)(batch * rows * cols) * s;
             const double t = half_cost(tile, tiles * s, (double)((steps + s - 1) / s)) + more;
             if (t < least) {
