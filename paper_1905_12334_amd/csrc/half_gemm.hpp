@@ -548,11 +548,6 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
 }
 struct HalfNothing {};
 
-template <class T, class F>
-__device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], const F &f) {
-    half_bands(at, acc, [](int, int) { return HalfNothing{}; }, [&](int r, int c, const float (&v)[8], HalfNothing) { f(r, c, v); }, [](int, float *) {});
-}
-
 // Results: with the canonical NaN.
 __device__ __forceinline__ u32x4 half_round8(const float v[8]) {
     u32x4 w;

@@ -217,7 +217,9 @@ __device__ __forceinline__ void xent_count_half(StatsAcc &st, float y) {
     st.zero_codes += (h & 0x7FFFu) == 0u ? 1u : 0u;
 }
 
-// A gradient, complete in its tile: unscaled, rounded and stored.  Rows of whole groups of eight.
+// A gradient, complete in its tile: unscaled, rounded and stored.  WHOLE: rows of whole groups of eight; others get a kernel of their own, whose
+// code is there once per band (four times, and the compiler keeps the accumulators in memory).
+template <bool WHOLE>
 struct XentOut : HalfNoneAhead {
     const int *exponent;
     float scale;
@@ -234,28 +236,60 @@ struct XentOut : HalfNoneAhead {
         const Philox rng(seed, offset);
         StatsAcc st;
         const uint32_t seen = stats != nullptr ? StatsAcc::peek(stats) : 0u;
-        half_bands(at, acc, [&](int r, int c, const float (&sum)[8]) {
+        half_bands<WHOLE ? 4 : 1>(at, acc, [](int, int) { return HalfNothing{}; }, [&](int r, int c, const float (&sum)[8], HalfNothing) {
             if (r >= rows || c >= cols) return;
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = sum[e] * unscale;
             const int64_t i = (row0 + r) * (int64_t)cols + c;
-            if (out16 != nullptr) *reinterpret_cast<u32x4 *>(out16 + i) = half_round8(v);
+            const int n = cols - c;  // of the eight, those that exist
+            if (out16 != nullptr) {
+                const u32x4 h = half_round8(v);
+                if constexpr (WHOLE) {
+                    *reinterpret_cast<u32x4 *>(out16 + i) = h;
+                } else if (n >= 8) {
+                    __builtin_memcpy(out16 + i, &h, 16);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n) out16[i + e] = (uint16_t)(h[e >> 1] >> (16 * (e & 1)));
+                }
+            }
             if (out8 != nullptr) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (sr) w = rng.block((uint64_t)i >> 3);
+                if (sr && WHOLE) {
+                    w = rng.block((uint64_t)i >> 3);
+                } else if (sr) {
+                    const Words4 a = rng.words_at((uint64_t)i), b = rng.words_at((uint64_t)i + 4);
+                    w = make_uint4(a.r01, a.r23, b.r01, b.r23);
+                }
                 const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
                 const u32x2 o = {e5m2_pack4_rt(lo, w.x, w.y, sr != 0, sat != 0), e5m2_pack4_rt(hi, w.z, w.w, sr != 0, sat != 0)};
-                *reinterpret_cast<u32x2 *>(out8 + i) = o;
+                if constexpr (WHOLE) {
+                    *reinterpret_cast<u32x2 *>(out8 + i) = o;
+                } else if (n >= 8) {
+                    __builtin_memcpy(out8 + i, &o, 8);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n) out8[i + e] = (uint8_t)(o[e >> 2] >> (8 * (e & 3)));
+                }
                 if (stats != nullptr) {
-                    st.add4(lo, o.x);
-                    st.add4(hi, o.y);
+                    if (WHOLE || n >= 8) {
+                        st.add4(lo, o.x);
+                        st.add4(hi, o.y);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 7; ++e)
+                            if (e < n) st.add1(v[e], (o[e >> 2] >> (8 * (e & 3))) & 0xFFu);
+                    }
                 }
             } else if (stats != nullptr) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) xent_count_half(st, v[e]);
+                for (int e = 0; e < 8; ++e)
+                    if (WHOLE || e < n) xent_count_half(st, v[e]);
             }
-        });
+        }, [](int, float *) {});
         if (stats != nullptr) {
             __syncthreads();  // (the bands' LDS)
             st.flush(stats, seen, reinterpret_cast<uint32_t (*)[16]>(at.lds));
@@ -302,6 +336,14 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
     }
 }
 
+// Wide accesses at addresses of any alignment.
+template <class V, bool ALIGNED>
+__device__ __forceinline__ V xent_load(const void *p) {
+    if constexpr (ALIGNED) return *reinterpret_cast<const V *>(p);
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
 // dst <- src [rows, cols] halves or 8-bit codes, as halves in panels, zeros up to the `wide` columns of the last one, tr threads per row; rows whose target is none are
 // zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).  VEC: rows of
 // whole, aligned groups of eight.  factor, where given, becomes that of a call without token weights.
@@ -319,24 +361,19 @@ __global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__
     }
     for (int c = c0; c < wide; c += 8 * tr) {
         u32x4 o = {0, 0, 0, 0};
-        if (live) {
-            if (VEC) {
-                if (c < cols) {
-                    if (CODES) {
-                        const u32x2 w = *reinterpret_cast<const u32x2 *>((const uint8_t *)src + r * ld_src + c);
-                        o = __builtin_bit_cast(u32x4, halves_of((int)w.x, (int)w.y));
-                    } else {
-                        o = *reinterpret_cast<const u32x4 *>((const uint16_t *)src + r * ld_src + c);
-                    }
+        if (live && c < cols) {
+            const auto *from = (const uint8_t *)src + (r * ld_src + c) * (CODES ? 1 : 2);
+            if (c + 8 <= cols) {
+                if (CODES) {
+                    const u32x2 w = xent_load<u32x2, VEC>(from);
+                    o = __builtin_bit_cast(u32x4, halves_of((int)w.x, (int)w.y));
+                } else {
+                    o = xent_load<u32x4, VEC>(from);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    uint32_t h = 0;
-                    if (c + e < cols)
-                        h = CODES ? (uint32_t)((const uint8_t *)src)[r * ld_src + c + e] << 8 : ((const uint16_t *)src)[r * ld_src + c + e];
-                    o[e >> 1] |= h << (16 * (e & 1));
-                }
+                for (int e = 0; e < 7; ++e)
+                    if (c + e < cols) o[e >> 1] |= (CODES ? (uint32_t)from[e] << 8 : ((const uint16_t *)from)[e]) << (16 * (e & 1));
             }
         }
         *reinterpret_cast<u32x4 *>(dst + HalfMatrix::at(r, c, 64 * (int64_t)rows)) = o;
@@ -396,7 +433,15 @@ __global__ __launch_bounds__(256) void xent_finish_kernel(const XentFinish p, in
     for (int64_t r = (int64_t)blockIdx.x * per + threadIdx.x / tr; r < p.rows; r += (int64_t)gridDim.x * per) {
         for (int64_t c = 4 * (threadIdx.x % tr); c < p.cols; c += 4 * tr) {
             f32x4 v = *reinterpret_cast<const f32x4 *>(p.sum + r * p.ld + c);
-            for (int s = 1; s < p.slabs; ++s) v += *reinterpret_cast<const f32x4 *>(p.sum + s * p.slab + r * p.ld + c);
+            // (eight loads under way: one by one the 64 slabs of 12 x 460 took 26 us)
+            const float *from = p.sum + r * p.ld + c;
+            for (int s = 1; s < p.slabs; s += 8) {
+                f32x4 more[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) more[u] = s + u < p.slabs ? *reinterpret_cast<const f32x4 *>(from + (s + u) * p.slab) : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int u = 0; u < 8; ++u) v += more[u];
+            }
             const float y[4] = {v.x * unscale, v.y * unscale, v.z * unscale, v.w * unscale};
             const int64_t at = (p.row0 + r) * p.cols + c;
             const int n = p.cols - c < 4 ? (int)(p.cols - c) : 4;
@@ -499,8 +544,8 @@ int parts_of(const Shape &s) {  // sums per token
     }
     return n;
 }
-// dx and dw.  A tile that holds the complete sum stores the gradient itself where a row is whole groups of eight; otherwise FP32 sums
-// (of every slice; of all pieces, for dx) pass through the workspace.
+// dx and dw.  A tile that holds the complete sum stores the gradient itself; otherwise FP32 sums (of every slice; of all pieces, for dx) pass
+// through the workspace.
 struct BwdPlans {
     HalfPlan dx, dw;
     bool dx_direct, dw_direct;
@@ -509,8 +554,8 @@ BwdPlans bwd_plans(const Shape &s) {
     BwdPlans p;
     p.dx = half_plan(1, s.M, s.K, s.piece, false, 64);
     p.dw = half_plan(1, s.piece, s.K, s.M, false, 64);
-    p.dx_direct = s.K % 8 == 0 && p.dx.splits == 1 && s.piece >= s.N;
-    p.dw_direct = s.K % 8 == 0 && p.dw.splits == 1;
+    p.dx_direct = p.dx.splits == 1 && s.piece >= s.N;
+    p.dw_direct = p.dw.splits == 1;
     return p;
 }
 Layout make_layout(const Shape &s, bool backward, bool dx, bool dw) {
@@ -668,8 +713,12 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
     auto direct = [&](auto atn, int tile, const HalfMatrix &a, const HalfMatrix &b, int64_t rows, int64_t kc, int64_t row0, uint16_t *out16,
                       uint8_t *out8, uint64_t offset, mp8_stats *stats) {
         constexpr bool ATN = decltype(atn)::value;
-        const XentOut epi{{}, exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0, seed, offset, stats};
-        return product<true, ATN>(tile, a, b, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
+        auto run = [&](auto whole) {
+            const XentOut<decltype(whole)::value> epi{{}, exponent, scale, (int)rows, (int)K, row0, out16, out8, round == MP8_SR, (flags & MP8_FLAG_SATURATE) != 0,
+                                                      seed, offset, stats};
+            return product<true, ATN>(tile, a, b, ATN ? up(rows, 8) : rows, K8, kc, 1, epi, st);
+        };
+        return K % 8 == 0 ? run(std::true_type{}) : run(std::false_type{});
     };
     for (int64_t c = 0; c < N; c += s.piece) {
         const int64_t cols = N - c < s.piece ? N - c : s.piece;
