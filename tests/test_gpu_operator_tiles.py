@@ -75,7 +75,8 @@ def within(got, want, bound, what):
 @pytest.mark.parametrize("M,N,K", [(2055, 4099, 136), (3001, 9001, 72), (4099, 8200, 520), (1111, 40009, 264), (9001, 1999, 1032), (512, 20001, 2056),
                                    (8200, 40001, 40), (921, 16507, 386), (893, 18915, 472), (1, 34847, 136), (1, 36418, 135), (1215, 14131, 16),
                                    (22139, 2, 2032), (15981, 937, 16), (33505, 2, 8), (37658, 2, 144), (34686, 756, 256), (1, 76922, 1), (35368, 2, 1),
-                                   (21873, 2, 324), (33885, 858, 194)])
+                                   (21873, 2, 324), (33885, 858, 194), (8709, 31376, 1), (1, 33607, 1), (10116, 5634, 134), (19893, 395, 4304),
+                                   (15724, 6555, 1), (9620, 9091, 400)])
 def test_cross_entropy_of_large_tiles(mp8, M, N, K):
     x, w, t = inputs(M + N, M, N, K)
     scale = 256.0 / M
@@ -170,7 +171,8 @@ def momentum(mp8, w, v, g, lr, **kw):
     (54, 2, 896), (21, 1, 10872), (43, 259, 283), (3, 1128, 1413), (41, 575, 712), (8, 920, 5333), (16, 1001, 1032), (1, 2956, 13518), (1, 835, 901),
     (1, 854, 835), (13, 2732, 134), (16, 132, 2134), (1, 865, 9807), (1, 8478, 994),
     (1, 64, 64), (70, 64, 1000), (70, 1000, 64), (1, 127, 129), (1, 129, 127), (6, 128, 700), (6, 700, 128), (9, 128, 4000), (2, 160, 1000), (2, 1000, 185),
-    (1, 192, 192), (1, 193, 255), (3, 256, 256), (1, 3000, 249), (1, 250, 9000)])
+    (1, 192, 192), (1, 193, 255), (3, 256, 256), (1, 3000, 249), (1, 250, 9000), (1, 2313, 2016), (13, 6244, 519),
+    (5, 846, 2519)])
 def test_direction_of_large_tiles(mp8, batch, rows, cols):
     gen = torch.Generator(device="cuda").manual_seed(rows + cols)
     g = codes(torch.randn((batch, rows, cols), generator=gen, device="cuda"))
