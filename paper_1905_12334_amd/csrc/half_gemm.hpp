@@ -472,6 +472,13 @@ __device__ __forceinline__ u32x4 half_operand8(const float v[8]) {
     return __builtin_bit_cast(u32x4, h);
 }
 
+// The bands are private to a wave, whose LDS accesses are carried out in order: what one lane writes and another reads has to stay in it.
+__device__ __forceinline__ void half_wave_lds() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Rows of halves through LDS, so that a store covers whole 128-byte lines (pieces of 32 bytes, as the accumulators lie, kept the L2 busy
 // for as long as four times their size: 8192 x 32768 halves in 256x256 tiles 9 us per round of tiles).  A band of 32 rows of a wave's
 // part takes WTN * 64 bytes; 16-byte chunk c of row r sits in slot c ^ (r & mask), and its halves change places in rows 16 .. 31, which
@@ -491,6 +498,7 @@ struct HalfLines {
     template <class F>
     __device__ __forceinline__ void each(const F &f) {
         const int lr = lane / PER, c = lane % PER;
+        half_wave_lds();
 #pragma unroll
         for (int k = 0; k < PASSES; ++k) {
             const int r = ROWS * k + lr;
@@ -498,6 +506,7 @@ struct HalfLines {
             const u32x4 v = *reinterpret_cast<const u32x4 *>(band + r * T::WTN * 2 + ((c ^ (r & MASK)) << 4));
             f(r, 8 * c, r < 16 ? v : u32x4{v.z, v.w, v.x, v.y});
         }
+        half_wave_lds();
     }
 };
 
@@ -525,6 +534,7 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
                 const f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
                 *reinterpret_cast<f32x4 *>(band + (at.lane & 31) * PITCH + 32 * j + 8 * g + 4 * (at.lane >> 5)) = v;
             }
+        half_wave_lds();
         const int r0 = at.row0 + 32 * i, c = at.col0 + lc;
 #pragma unroll 1
         for (int q = 0; q < PASSES; q += U) {
@@ -544,6 +554,7 @@ __device__ __forceinline__ void half_bands(const HalfPlace<T> &at, f32x16 (&acc)
                 f(r0 + k, c, v, x[u]);
             }
         }
+        half_wave_lds();
     }
 }
 struct HalfNothing {};

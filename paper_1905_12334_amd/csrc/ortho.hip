@@ -63,6 +63,7 @@ __device__ __forceinline__ void ortho_bands(const HalfPlace<T> &at, f32x16 (&acc
     }, [&](int i, float *band) {
         if constexpr (!TALL) {
             if (at.lane < 32) band[at.lane * kHalfBandPitch<T> + T::WTN] = in.d[i];
+            half_wave_lds();
             rows = band + T::WTN;
         }
     });
