@@ -20,6 +20,14 @@
 
 namespace mp8 {
 
+// Wide accesses at addresses of any alignment, which cost as much as others where they are aligned.
+template <class V>
+__device__ __forceinline__ V any_aligned(const void *p) {
+    V v;
+    __builtin_memcpy(&v, p, sizeof(V));
+    return v;
+}
+
 constexpr float kOrthoA = 3.4445f, kOrthoB = -4.7750f, kOrthoC = 2.0315f;
 constexpr float kUp = 16384.0f, kDown = 1.0f / 16384.0f;  // the scale of A and of the polynomial
 
@@ -220,11 +228,11 @@ struct OrthoUpdate {
             if (r >= rows || c >= cols) return in;
             in.x = *reinterpret_cast<const u32x4 *>(x + at.batch * batch + HalfMatrix::at(r, c, panel));
             const int64_t i0 = first + (int64_t)r * cols + c;
-            if (whole) {
-                in.w = *reinterpret_cast<const u32x4 *>(w16 + i0);
+            if (whole || c + 8 <= cols) {
+                in.w = any_aligned<u32x4>(w16 + i0);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 7; ++e)
                     if (c + e < cols) in.w[e >> 1] |= (uint32_t)w16[i0 + e] << (16 * (e & 1));
             }
             return in;
@@ -259,12 +267,12 @@ struct OrthoUpdate {
             }
             const uint32_t lo[2] = {o.x, o.y}, hi[2] = {o.z, o.w};
             const u32x2 codes = {w8 != nullptr ? e5m2_of_halves(lo) : 0u, w8 != nullptr ? e5m2_of_halves(hi) : 0u};
-            if (whole) {
-                *reinterpret_cast<u32x4 *>(w16 + i0) = o;
-                if (w8 != nullptr) *reinterpret_cast<u32x2 *>(w8 + i0) = codes;
+            if (n == 8) {
+                __builtin_memcpy(w16 + i0, &o, 16);
+                if (w8 != nullptr) __builtin_memcpy(w8 + i0, &codes, 8);
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
+                for (int e = 0; e < 7; ++e)
                     if (e < n) {
                         w16[i0 + e] = (uint16_t)(o[e >> 1] >> (16 * (e & 1)));
                         if (w8 != nullptr) w8[i0 + e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
@@ -445,36 +453,32 @@ __global__ __launch_bounds__(256) void ortho_momentum_kernel(const OrthoMomentum
     const int64_t base = (int64_t)blockIdx.y * p.n;
     const int64_t per = (((p.n + p.blocks - 1) / p.blocks) + 3) & ~(int64_t)3;
     const int64_t first = blockIdx.x * per, end = first + per < p.n ? first + per : p.n;
-    // (a matrix may start anywhere: groups of four by address)
     double sum = 0.0;
     uint32_t nonfinite = 0;
-    auto one = [&](int64_t i) {
-        const uint32_t code = p.g8[base + i];
-        nonfinite += (code & 0x7Cu) == 0x7Cu ? 1u : 0u;
-        if (skipping) return;
+    auto one = [&](uint32_t code, float v) {
         const float g = e5m2_to_f32(code) * p.inv_scale;
-        const float v = __builtin_fmaf(p.mu, p.v[base + i], g);
-        p.v[base + i] = v;
+        v = __builtin_fmaf(p.mu, v, g);
         const double u = (double)ortho_direction(v, g, p.mu, p.nesterov);
         sum += u * u;
+        return v;
     };
-    if (((base | p.n) & 3) == 0) {
-        for (int64_t i = first + 4 * threadIdx.x; i < end; i += 1024) {
-            const uint32_t codes = *reinterpret_cast<const uint32_t *>(p.g8 + base + i);
+    // (a matrix may start anywhere: 2001 x 1013 took 11.4 us element by element, 1024 x 4096 8.1)
+    for (int64_t i = first + 4 * threadIdx.x; i < end; i += 1024) {
+        if (i + 4 <= end) {
+            const uint32_t codes = any_aligned<uint32_t>(p.g8 + base + i);
             nonfinite += __builtin_popcount(((codes & 0x7C7C7C7Cu) + 0x04040404u) & 0x80808080u);
             if (skipping) continue;
-            f32x4 v = *reinterpret_cast<const f32x4 *>(p.v + base + i);
+            f32x4 v = any_aligned<f32x4>(p.v + base + i);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float g = e5m2_to_f32((codes >> (8 * e)) & 0xFFu) * p.inv_scale;
-                v[e] = __builtin_fmaf(p.mu, v[e], g);
-                const double u = (double)ortho_direction(v[e], g, p.mu, p.nesterov);
-                sum += u * u;
+            for (int e = 0; e < 4; ++e) v[e] = one((codes >> (8 * e)) & 0xFFu, v[e]);
+            __builtin_memcpy(p.v + base + i, &v, 16);
+        } else {
+            for (int64_t k = base + i; k < base + end; ++k) {
+                const uint32_t code = p.g8[k];
+                nonfinite += (code & 0x7Cu) == 0x7Cu ? 1u : 0u;
+                if (!skipping) p.v[k] = one(code, p.v[k]);
             }
-            *reinterpret_cast<f32x4 *>(p.v + base + i) = v;
         }
-    } else {
-        for (int64_t i = first + threadIdx.x; i < end; i += 256) one(i);
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
@@ -505,7 +509,6 @@ struct OrthoStart {
 __global__ __launch_bounds__(256) void ortho_start_kernel(const OrthoStart p) {
     const uint32_t groups = (uint32_t)p.rows * p.div_groups.d, stride = gridDim.x * 256;
     const int64_t base = (int64_t)blockIdx.y * p.rows * p.cols;
-    const bool whole = (p.cols & 7) == 0;
     if (p.skip != nullptr && *p.skip != 0u) return;
     double sum = 0.0;  // (by all lanes of the wave, also those without a group)
     for (int b = threadIdx.x & 63; b < p.blocks; b += 64) sum += p.squares[(int64_t)blockIdx.y * p.blocks + b];
@@ -519,9 +522,9 @@ __global__ __launch_bounds__(256) void ortho_start_kernel(const OrthoStart p) {
         const int64_t i = base + (int64_t)r * p.cols + c;
         uint32_t code[2] = {0, 0};
         float v[8];
-        if (whole) {
-            const u32x2 g = *reinterpret_cast<const u32x2 *>(p.g8 + i);
-            const f32x4 a = *reinterpret_cast<const f32x4 *>(p.v + i), b = *reinterpret_cast<const f32x4 *>(p.v + i + 4);
+        if (c + 8 <= p.cols) {
+            const u32x2 g = any_aligned<u32x2>(p.g8 + i);
+            const f32x4 a = any_aligned<f32x4>(p.v + i), b = any_aligned<f32x4>(p.v + i + 4);
             code[0] = g.x;
             code[1] = g.y;
 #pragma unroll
