@@ -102,6 +102,21 @@ struct Philox {
         return {__builtin_amdgcn_alignbit(w[1], w[0], (h & 1) * 16), __builtin_amdgcn_alignbit(w[2], w[1], (h & 1) * 16)};
     }
 
+    // The words of elements i .. i+7 for any i (two blocks; two calls of words_at come to four).
+    __device__ __forceinline__ uint4 eight_at(uint64_t i) const {
+        const uint4 a = block(i >> 3), b = block((i >> 3) + 1);
+        const int h = (int)(i & 7);
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        const uint32_t m4 = (h & 4) ? ~0u : 0u, m2 = (h & 2) ? ~0u : 0u;
+#pragma unroll
+        for (int j = 0; j < 6; ++j) w[j] = (w[j + 2] & m4) | (w[j] & ~m4);
+#pragma unroll
+        for (int j = 0; j < 5; ++j) w[j] = (w[j + 1] & m2) | (w[j] & ~m2);
+        const int odd = (h & 1) * 16;
+        return make_uint4(__builtin_amdgcn_alignbit(w[1], w[0], odd), __builtin_amdgcn_alignbit(w[2], w[1], odd), __builtin_amdgcn_alignbit(w[3], w[2], odd),
+                          __builtin_amdgcn_alignbit(w[4], w[3], odd));
+    }
+
     // Lanes 2m and 2m + 1 need the first and the second half of block `a`, and of block `b` (the same
     // for both lanes): the even lane computes a, the odd one b, and each hands over the other's half.
     // Every lane of the wave must be active.

@@ -243,13 +243,8 @@ struct OrthoUpdate {
             const u32x4 xw = in.x, ww = in.w;
             uint32_t rw[4] = {0, 0, 0, 0};
             if (sr) {
-                if (whole) {
-                    const uint4 b = rng.block((uint64_t)i0 >> 3);
-                    rw[0] = b.x; rw[1] = b.y; rw[2] = b.z; rw[3] = b.w;
-                } else {
-                    const Words4 a = rng.words_at((uint64_t)i0), b = rng.words_at((uint64_t)i0 + 4);
-                    rw[0] = a.r01; rw[1] = a.r23; rw[2] = b.r01; rw[3] = b.r23;
-                }
+                const uint4 b = whole ? rng.block((uint64_t)i0 >> 3) : rng.eight_at((uint64_t)i0);
+                rw[0] = b.x; rw[1] = b.y; rw[2] = b.z; rw[3] = b.w;
             }
             u32x4 o;
 #pragma unroll

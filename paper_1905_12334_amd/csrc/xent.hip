@@ -257,12 +257,7 @@ struct XentOut : HalfNoneAhead {
             }
             if (out8 != nullptr) {
                 uint4 w = make_uint4(0u, 0u, 0u, 0u);
-                if (sr && WHOLE) {
-                    w = rng.block((uint64_t)i >> 3);
-                } else if (sr) {
-                    const Words4 a = rng.words_at((uint64_t)i), b = rng.words_at((uint64_t)i + 4);
-                    w = make_uint4(a.r01, a.r23, b.r01, b.r23);
-                }
+                if (sr) w = WHOLE ? rng.block((uint64_t)i >> 3) : rng.eight_at((uint64_t)i);
                 const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
                 const u32x2 o = {e5m2_pack4_rt(lo, w.x, w.y, sr != 0, sat != 0), e5m2_pack4_rt(hi, w.z, w.w, sr != 0, sat != 0)};
                 if constexpr (WHOLE) {
