@@ -514,15 +514,16 @@ struct Layout {
     size_t factor, exponent, e, dx, dw, total;  // backward: (copies as above,) the tokens' factors, e, FP32 sums
 };
 // The logits' tiles: their epilogues take longer than others, and two workgroups per CU hide them behind each other's products.  Measured,
-// us, statistics in 256x256 / 128x128 tiles: 4096 x 32000 x 512 160 / 155, 8192 x 32768 x 2048 905 / 1032; the errors 184 / 183, 958 / 1109.
+// us, statistics in 256x256 / 128x128 tiles: 9243 x 24384 x 64 166 / 124, 8192 x 32000 x 256 267 / 238, 4096 x 32000 x 512 216 / 211,
+// 1021 x 32003 x 1000 85 / 102, 8192 x 32768 x 2048 905 / 1032; the errors 206 / 149, 304 / 279, 235 / 222, 87 / 96, 958 / 1109.
 HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
     HalfPlan best = half_plan(1, M, cols, K, false, 1);
     if (best.tile == 64) return best;
     double least = 1e300;
     for (const int tile : {256, 128}) {
-        const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 8.0 : 4.0;
+        const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 8.0 : 2.2;
         const double rounds = std::ceil((double)(((M + tile - 1) / tile) * ((cols + tile - 1) / tile)) / slots);
-        const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.6 : 0.97) + (rounds + 1.0) * epilogue;
+        const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.6 : 1.05) + (rounds + 1.0) * epilogue;
         if (t < least) {
             least = t;
             best.tile = tile;
