@@ -76,7 +76,7 @@ def within(got, want, bound, what):
                                    (8200, 40001, 40), (921, 16507, 386), (893, 18915, 472), (1, 34847, 136), (1, 36418, 135), (1215, 14131, 16),
                                    (22139, 2, 2032), (15981, 937, 16), (33505, 2, 8), (37658, 2, 144), (34686, 756, 256), (1, 76922, 1), (35368, 2, 1),
                                    (21873, 2, 324), (33885, 858, 194), (8709, 31376, 1), (1, 33607, 1), (10116, 5634, 134), (19893, 395, 4304),
-                                   (15724, 6555, 1), (9620, 9091, 400)])
+                                   (15724, 6555, 1), (9620, 9091, 400), (2500, 20003, 1999)])
 def test_cross_entropy_of_large_tiles(mp8, M, N, K):
     x, w, t = inputs(M + N, M, N, K)
     scale = 256.0 / M
