@@ -609,10 +609,10 @@ struct HalfPlan {
     int tile, splits;
 };
 
-// Estimated time, us, of `tiles` tiles over `stages` stages.  Measured (4096 x 4096 x 4096 and parts of it), us per stage: 64x64 tiles, up to 256
-// of them 0.26 (kByIndex 0.19), 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93 (1.08 over long contractions, as
-// the clock sinks: 6007 x 1000 over 37003 536 us, in 256x256 tiles, estimated slower with 0.93, 418); 192x192, 64 0.81, 256 1.06; 256x256, 128 1.36, 256 1.73; more tiles
-// take rounds.  On top come start and end of a workgroup.
+// Estimated time, us, of `tiles` tiles over `stages` stages.  Measured (4096 x 4096 x 4096 and parts of it), us per stage: 64x64 tiles, up to
+// 256 of them 0.26 (kByIndex 0.19), 512 (two per CU) 0.41; 128x128, 256 0.69, 512 0.93 (1.08 over long contractions, as the clock sinks:
+// 6007 x 1000 over 37003 536 us; in 256x256 tiles, estimated slower with 0.93, 418); 192x192, 64 0.81, 256 1.06; 256x256, 128 1.36,
+// 256 1.73; more tiles take rounds.  On top come start and end of a workgroup.
 static inline double half_cost(int tile, int64_t tiles, double stages) {
     const int64_t slots = tile > 128 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
     const double whole = tile == 256 ? 1.73 : tile == 192 ? 1.06 : tile == 128 ? 1.08 : 0.41, half = tile == 256 ? 1.36 : tile == 192 ? 0.85 : tile == 128 ? 0.69 : 0.25;

@@ -7,13 +7,13 @@
 // A step maps every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors alone: with (a, b, c) = (3.4445,
 // -4.7750, 2.0315), whose slope at zero is steep, five steps bring all but the smallest to 0.7 .. 1.2.
 //
-// X has the weights' rows and columns, in panels of 64 columns, and so have A and the polynomial.  A is formed over the shorter side: X X^T and (bA + cA^2) X where rows <= cols, X^T X and
-// X (bA + cA^2) otherwise; the second product of the last step updates the weights itself.  Operands of the products are
-// halves, sums FP32.  A power of two keeps each of them in the format's range: singular values stay below 1.21, so that entries of A
-// are below 1.46 and those of bA + cA^2 below 2.81 in magnitude; A and the polynomial are stored times 2^14, X times S = 2^round(log2
-// sqrt n), which makes the entries of an orthogonal X about 1.  What half operands cost: entries of X are off by 1.3e-3 of
-// their root mean square after five steps from a Gaussian u, 1.4e-2 where eight directions hold nearly all of it (bfloat16
-// operands: 1e-2 and 0.11; FP32: 1.3e-6 and 5e-6).
+// X has the weights' rows and columns, in panels of 64 columns, and so have A and the polynomial.  A is formed over the shorter side:
+// X X^T and (bA + cA^2) X where rows <= cols, X^T X and X (bA + cA^2) otherwise; the second product of the last step updates the weights
+// itself.  Operands of the products are halves, sums FP32.  A power of two keeps each of them in the format's range: singular values stay
+// below 1.21, so that entries of A are below 1.46 and those of bA + cA^2 below 2.81 in magnitude; A and the polynomial are stored times
+// 2^14, X times S = 2^round(log2 sqrt n), which makes the entries of an orthogonal X about 1.  What half operands cost: entries of X are off
+// by 0.7e-3 to 1.2e-3 of their root mean square after five steps from a Gaussian u (ortho_combine), some 1e-2 where eight directions hold
+// nearly all of it (bfloat16 operands: 1e-2 and 0.11; FP32: 1.3e-6 and 5e-6).
 #include <cmath>
 
 #include "half_gemm.hpp"

@@ -339,9 +339,9 @@ __device__ __forceinline__ V xent_load(const void *p) {
     __builtin_memcpy(&v, p, sizeof(V));
     return v;
 }
-// dst <- src [rows, cols] halves or 8-bit codes, as halves in panels, zeros up to the `wide` columns of the last one, tr threads per row; rows whose target is none are
-// zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as 0 x NaN).  VEC: rows of
-// whole, aligned groups of eight.  factor, where given, becomes that of a call without token weights.
+// dst <- src [rows, cols] halves or 8-bit codes, as halves in panels, zeros up to the `wide` columns of the last one, tr threads per row; rows
+// whose target is none are zero too where targets are given (what a padded token holds must not reach the weights' gradient, not even as
+// 0 x NaN).  VEC: rows of whole, aligned groups of eight.  factor, where given, becomes that of a call without token weights.
 template <bool CODES, bool VEC>
 __global__ __launch_bounds__(256) void xent_copy_kernel(const void *__restrict__ src, int64_t ld_src, uint16_t *__restrict__ dst, int wide,
                                                         int rows, int cols, const int64_t *__restrict__ targets, int N, int tr,
