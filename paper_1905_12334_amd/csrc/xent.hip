@@ -324,8 +324,8 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
         loss[r] = 0.0f;
     } else {
         const double z = (double)z_target[r], d = (double)t.x - z * 1.4426950408889634074;
-        // log(1 + sum 2^d)
-        const double l = d < 900.0 ? log1p((double)t.y * exp2(d)) : kLn2 * (d + log2((double)t.y));
+        // log(1 + sum 2^d); with nothing beside the target the base means nothing, and the loss is 0 (NaN where the logit is)
+        const double l = t.y == 0.0f ? z - z : d < 900.0 ? log1p((double)t.y * exp2(d)) : kLn2 * (d + log2((double)t.y));
         loss[r] = (float)l;
         lse[r] = (float)(z + l);
     }

@@ -1,0 +1,51 @@
+"""GPU tests of the softmax cross entropy where its softmax degenerates: nothing beside the target, logits without bounds, logits that are
+large and close to each other.  Bounds as derived in test_gpu_softmax_xent.py."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_softmax_xent import H, U, backward, buffers, close, forward, mp8, truth  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def tokens(x, w, t):
+    """The inputs of a call, halves as given."""
+    (M, K), N = x.shape, w.shape[0]
+    return dict(M=M, N=N, K=K, ldx=K, ldw=K, x=x.astype(np.float16), w=w.astype(np.float16), t=np.asarray(t, np.int64), dloss=None, x8=False)
+
+
+def logits(z, N, K=8):
+    """Tokens whose first logit is z and whose others are what w's rows make of them: x is one in its first feature."""
+    x, w = np.zeros((len(z), K)), np.zeros((N, K))
+    x[:, 0], w[0, 0] = 1.0, z[0]
+    return x, w
+
+
+@pytest.mark.parametrize("M", [1, 70, 600])
+@pytest.mark.parametrize("z", [-60000.0, -1000.0, -600.0, 0.0, 1000.0])
+def test_one_class(mp8, M, z):
+    """Nothing stands beside the target: the loss is 0 and lse the logit, wherever it lies, and there is no gradient."""
+    x, w = logits([z] * M, 1)
+    t = np.zeros(M)
+    t[1::5] = -1
+    c = tokens(x, w, t)
+    x, w, t, loss, lse = forward(mp8, c)
+    live = t == 0
+    assert not loss.any()
+    assert bool((lse[live] == z).all()) and bool(((lse - z).abs() <= 4 * U * abs(z)).all())
+    dx, dw = buffers(M, 1, 8, torch.float16)
+    stats = mp8.new_stats()
+    backward(mp8, c, x, w, t, loss, lse, scale=1024.0, dx16=dx[:M * 8], dw16=dw[:8], dx_stats=stats, dw_stats=stats)
+    assert not dx[:M * 8].any() and not dw[:8].any() and mp8.read_stats(stats) == (0, 0, 0)
+
+
+def test_other_classes_without_probability(mp8):
+    """Logits of minus infinity beside the target's."""
+    for z in (-1000.0, -2.0, 1000.0):
+        x, w = logits([z] * 3, 200)
+        w[1:, 0] = -np.inf
+        loss, lse = forward(mp8, tokens(x, w, [0, 0, 0]))[3:]
+        assert not loss.any() and bool((lse == z).all())
