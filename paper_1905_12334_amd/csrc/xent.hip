@@ -324,10 +324,19 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
         loss[r] = 0.0f;
     } else {
         const double z = (double)z_target[r], d = (double)t.x - z * 1.4426950408889634074;
-        // log(1 + sum 2^d); with nothing beside the target the base means nothing, and the loss is 0 (NaN where the logit is)
-        const double l = t.y == 0.0f ? z - z : d < 900.0 ? log1p((double)t.y * exp2(d)) : kLn2 * (d + log2((double)t.y));
+        double l, all;
+        if (t.y == 0.0f || z == (double)__builtin_inff()) {  // nothing beside the target: 0, but for a logit that is not finite
+            l = z - z;
+            all = z;
+        } else if (d >= 900.0) {  // nothing but the others
+            all = kLn2 * ((double)t.x + log2((double)t.y));
+            l = all - z;
+        } else {  // log(1 + sum 2^d)
+            l = log1p((double)t.y * exp2(d));
+            all = z + l;
+        }
         loss[r] = (float)l;
-        lse[r] = (float)(z + l);
+        lse[r] = (float)all;
     }
 }
 

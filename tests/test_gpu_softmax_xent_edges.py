@@ -49,3 +49,29 @@ def test_other_classes_without_probability(mp8):
         w[1:, 0] = -np.inf
         loss, lse = forward(mp8, tokens(x, w, [0, 0, 0]))[3:]
         assert not loss.any() and bool((lse == z).all())
+
+
+def test_infinite_logits(mp8):
+    """From the definition: a target at minus infinity leaves lse to the others (its loss is infinite), one at plus infinity has no loss, and a
+    row of nothing but infinities has none either; what is not a number stays so, whichever class it is."""
+    N, inf = 300, np.inf
+    rng = np.random.default_rng(2)
+    w = np.zeros((N, 8))
+    w[:, 0] = rng.standard_normal(N)
+    w = w.astype(np.float16).astype(np.float64)
+    w[0, 0], w[1, 0], w[2, 0] = inf, -inf, np.nan
+    x = np.zeros((1, 8))
+    x[0, 0] = 1.0
+    usual = [k for k in range(3, N)]
+    # classes, target among them, loss, lse
+    others = lambda keep: float(np.log(np.exp(w[keep, 0]).sum()))
+    for keep, target, loss, lse in ((usual, 5, others(usual) - w[usual[5], 0], others(usual)), (usual + [1], 5, others(usual) - w[usual[5], 0], others(usual)),
+                                    (usual + [1], len(usual), inf, others(usual)), (usual + [0], len(usual), np.nan, inf), ([0], 0, np.nan, inf),
+                                    ([1], 0, np.nan, -inf), (usual + [2], 5, np.nan, np.nan), (usual + [2], len(usual), np.nan, np.nan), ([2], 0, np.nan, np.nan)):
+        got = forward(mp8, tokens(x, w[keep], [target]))
+        r = (math.log(2) * 12 + 64 + N / 32 + 16) * U  # (products with zeros and one are exact)
+        for value, want, bound in ((float(got[3]), loss, r * abs(loss)), (float(got[4]), lse, r + 4 * U * abs(lse))):
+            if np.isfinite(want):
+                assert abs(value - want) <= bound, (target, value, want)
+            else:
+                assert value == want or (np.isnan(value) and np.isnan(want)), (target, value, want)
