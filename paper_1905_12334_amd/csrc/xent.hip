@@ -15,7 +15,6 @@
 namespace mp8 {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.69314718055994530942;
 // e is stored times 2^14: values of up to 1 in magnitude fill the half format from its top, and a probability keeps eleven bits
 // down to 2^-28 and an absolute precision of 2^-39 below.
 constexpr int kErrorExponent = 14;
@@ -320,16 +319,18 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const f32x2 *__restrict_
     if (y != 0 || r >= M) return;
     const int64_t target = targets[r];
     if (target < 0 || target >= N) {
-        lse[r] = (float)(kLn2 * ((double)t.x + log2((double)t.y)));
+        lse[r] = (float)(((double)t.x + log2((double)t.y)) / (double)kLog2e);
         loss[r] = 0.0f;
     } else {
-        const double z = (double)z_target[r], d = (double)t.x - z * 1.4426950408889634074;
+        // (log2 e as the tiles' sums have it, in FP32: with its other digits what all logits have in common would not cancel, 2e-4 of the loss
+        // at logits around 2^14)
+        const double z = (double)z_target[r], d = (double)t.x - z * (double)kLog2e;
         double l, all;
         if (t.y == 0.0f || z == (double)__builtin_inff()) {  // nothing beside the target: 0, but for a logit that is not finite
             l = z - z;
             all = z;
         } else if (d >= 900.0) {  // nothing but the others
-            all = kLn2 * ((double)t.x + log2((double)t.y));
+            all = ((double)t.x + log2((double)t.y)) / (double)kLog2e;
             l = all - z;
         } else {  // log(1 + sum 2^d)
             l = log1p((double)t.y * exp2(d));

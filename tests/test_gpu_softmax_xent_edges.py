@@ -75,3 +75,23 @@ def test_infinite_logits(mp8):
                 assert abs(value - want) <= bound, (target, value, want)
             else:
                 assert value == want or (np.isnan(value) and np.isnan(want)), (target, value, want)
+
+
+@pytest.mark.parametrize("common", [0.0, 2.0 ** 10, -2.0 ** 14, 2.0 ** 17, -2.0 ** 17])
+@pytest.mark.parametrize("M,N", [(3, 40), (130, 700), (700, 3000)])
+def test_a_part_that_all_logits_have_in_common_cancels(mp8, common, M, N):
+    """Logits in steps of 2^-6, exact in FP32 whatever they have in common (dz = 0), so that only the softmax's own roundings are left.  Differences
+    are scaled by an FP32 log2 e on one side and undone on the other: that is one more U of the spread."""
+    rng = np.random.default_rng(N)
+    x, w = np.zeros((M, 8)), np.zeros((N, 8))
+    x[:, 0], w[:, 0] = 512.0, common / 512.0
+    x[:, 1:3] = rng.integers(-2, 3, (M, 2))
+    w[:, 1:3] = rng.integers(-64, 65, (N, 2)) / 64.0
+    c = tokens(x, w, rng.integers(0, N, M))
+    z = x @ w.T
+    assert (z == z.astype(np.float32)).all()
+    want = truth(c)
+    r = (2 * math.log(2) * ((z.max(1) - z.min(1)) / math.log(2) + 1) + 64 + N / 32 + 16) * U
+    loss, lse = forward(mp8, c)[3:]
+    close(loss, want["loss"], want["loss"] * (r + 4 * U), "loss")
+    close(lse, want["lse"], r + 4 * U * np.abs(want["lse"]), "lse")
