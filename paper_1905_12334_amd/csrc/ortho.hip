@@ -77,6 +77,14 @@ __device__ __forceinline__ void ortho_bands(const HalfPlace<T> &at, f32x16 (&acc
     });
 }
 
+// Eight columns from c on, zeros where they do not exist.
+__device__ __forceinline__ void ortho_clear_behind(u32x4 &w, int c, int cols) {
+    if (cols - c >= 8) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (e >= cols - c) w[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
+}
+
 // A symmetric output of halves, made from its upper tiles: v = scale * acc (POLY: + linear * in[r, c]) at (r, c) and, off the diagonal's
 // tiles, at (c, r), turned round by the lanes that read the band.  Columns m .. m8 - 1 are zero.
 // With the conversions of the results' epilogues (canonical NaN, a test per element) two bands of a 128x128 tile took 5 us.
@@ -128,11 +136,7 @@ struct OrthoSymmetric {
             for (int e = 0; e < 8; ++e) v[e] = sum[e];
             value(xw, v);
             u32x4 w = half_operand8(v);
-            if (m - c < 8) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= m - c) w[e >> 1] &= e & 1 ? 0xFFFFu : 0xFFFF0000u;
-            }
+            ortho_clear_behind(w, c, m);
             *reinterpret_cast<u32x4 *>(o + HalfMatrix::at(r, c, panel)) = w;
         }, [&](int i, const float *band) {
             if (POLY && at.row0 == at.col0) {
@@ -164,7 +168,9 @@ struct OrthoSymmetric {
     }
 };
 
-// The next iterate, a X + scale * acc, as halves.  Columns up to the next multiple of eight are stored (they are zero).
+// The next iterate, a X + scale * acc, as halves.  Columns up to the next multiple of eight are stored, as zeros: TALL, the product has the
+// polynomial's last row there (rows behind it are read as that one), and left as they are these columns grow by a factor of a per step,
+// to infinity in ten.
 template <bool TALL>
 struct OrthoNext {
     static constexpr bool kJoin = false, k192 = true;
@@ -191,7 +197,9 @@ struct OrthoNext {
             float v[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = ortho_combine(d[e], (float)h[e], sum[e]);
-            *reinterpret_cast<u32x4 *>(out + base + HalfMatrix::at(r, c, panel)) = half_operand8(v);
+            u32x4 w = half_operand8(v);
+            if constexpr (TALL) ortho_clear_behind(w, c, cols);
+            *reinterpret_cast<u32x4 *>(out + base + HalfMatrix::at(r, c, panel)) = w;
         });
     }
 };
