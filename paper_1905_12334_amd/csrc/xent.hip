@@ -531,8 +531,10 @@ HalfPlan logits_plan(int64_t M, int64_t cols, int64_t K) {
     if (best.tile == 64) return best;
     double least = 1e300;
     for (const int tile : {256, 128}) {
+        const int64_t tiles = ((M + tile - 1) / tile) * ((cols + tile - 1) / tile);
+        if (tiles > (int64_t)1 << 23) continue;  // (of 128x128 only: check_sizes; a launch holds less than 2^32 threads)
         const double slots = tile == 256 ? 256.0 : 512.0, epilogue = tile == 256 ? 8.0 : 2.2;
-        const double rounds = std::ceil((double)(((M + tile - 1) / tile) * ((cols + tile - 1) / tile)) / slots);
+        const double rounds = std::ceil((double)tiles / slots);
         const double t = rounds * (double)((K + 63) / 64) * (tile == 256 ? 1.6 : 1.05) + (rounds + 1.0) * epilogue;
         if (t < least) {
             least = t;

@@ -95,3 +95,18 @@ def test_a_part_that_all_logits_have_in_common_cancels(mp8, common, M, N):
     loss, lse = forward(mp8, c)[3:]
     close(loss, want["loss"], want["loss"] * (r + 4 * U), "loss")
     close(lse, want["lse"], r + 4 * U * np.abs(want["lse"]), "lse")
+
+
+@pytest.mark.parametrize("M,N,K", [(1 << 20, 1 << 19, 64), ((1 << 18) - 77, 1 << 21, 8)])
+def test_as_many_logits_as_a_launch_takes(mp8, M, N, K):
+    """About 2^23 tiles of 256x256, 2^39 logits: some tokens from all over, the last ones among them."""
+    import test_gpu_operator_tiles as tiles
+    x, w, t = tiles.inputs(1, M, N, K)
+    t[-1], t[-2] = N - 1, -1
+    loss, lse = torch.full((M,), 7.0, device="cuda"), torch.full((M,), 7.0, device="cuda")
+    mp8.softmax_xent_fwd_fp16(M, N, K, x, w, t, loss, lse, workspace=torch.empty(mp8.softmax_xent_fwd_workspace_bytes(M, N, K), dtype=torch.uint8, device="cuda"))
+    rows = torch.cat([torch.arange(0, M, M // 16, device="cuda"), torch.arange(M - 8, M, device="cuda")])
+    want = tiles.truth(x[rows].double(), w.double(), t[rows], 1.0)
+    tiles.within(lse[rows], want["lse"], want["dlse"], "lse")
+    tiles.within(loss[rows], want["loss"], want["loss"] * (want["r"] + 4 * U) + 1e-44, "loss")
+    assert bool((loss >= 0).all()) and bool(((lse > 0) & (lse < 100)).all())  # (every token has been written)
