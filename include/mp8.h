@@ -459,8 +459,10 @@ size_t mp8_softmax_xent_bwd_workspace_bytes(int64_t M, int64_t N, int64_t K, int
  *   skip_if_nonzero  as in mp8_sgd_update_fp16_sr; a flag inside *stats is refused (MP8_ERR_INVALID_ARG), since this call
  *              counts there while its later launches still read the flag
  * Other arguments as for mp8_sgd_momentum_fp16_sr.  A gradient code that is Inf or NaN makes its whole matrix NaN (unless the step is
- * skipped).  Precision: the velocity is FP32 as there; the products take half operands and add up in FP32, X is off by some 1e-3 of its
- * root mean square (0.7e-3 to 1.2e-3 for noise, 2e-3 with a few strong directions, 1e-2 where those hold nearly all of u).  Results are the same from run to run.
+ * skipped).  Precision: the velocity is FP32 as there; the products take half operands and add up in FP32.  X is off by 0.7e-3 to 1.2e-3 of
+ * its root mean square for noise.  Where k directions hold most of u it is up to 4e-3 with noise of a fifth of their size beside them, 7e-3
+ * with 0.05 (which 8-bit codes alone bring along), 2.5e-2 with 0.01 and 0.17 / sqrt(k) without any (FP32 operands: 1e-4): what the rounding of
+ * u to halves leaves in other directions grows with the steps as u's own parts do.  Results are the same from run to run.
  * rows, cols <= 2^20, batch <= 65535 and batch * rows / 64 * cols / 64 <= 2^23, rounded up (MP8_ERR_UNSUPPORTED beyond).  A zero
  * dimension is valid and does nothing.
  */
