@@ -425,12 +425,15 @@ mp8_status mp8_wgrad_adam_fp16_sr(int64_t M, int64_t N, int64_t K, const uint8_t
  *              element index).  What is not asked for is not computed; one at least is.
  *   dx_stats, dw_stats   nullable: of the 8-bit codes, or of the halves where only those are asked for
  *   workspace  device scratch, 16-byte aligned, mp8_softmax_xent_{fwd,bwd}_workspace_bytes(M, N, K, ldw) bytes; contents
- *              undefined afterwards.  Forward it grows with M * N / 8 bytes (large calls M * N / 32); backward it is bounded in N: the
- *              vocabulary is taken in pieces.
+ *              undefined afterwards.  Forward it grows with M * N / 8 bytes (large calls M * N / 32, with short rows of features / 16);
+ *              backward it is bounded in N: the vocabulary is taken in pieces.
  * Outputs overlap neither inputs nor each other.
  * Precision: logits, the softmax's sums and the gradients' sums are FP32 (the products' operands halves); e is rounded to half, times a power of two
  * that the largest token weight sets, before it is multiplied by w and x: eleven bits, which weights of less than 2^-14 of the
- * largest lose one by one.  The results are the same from run to run.
+ * largest lose one by one.  The loss does not depend on what all logits of a token have in common; the gradient's probabilities do, since
+ * lse is FP32: they are off by up to |lse| 2^-22 of themselves more.  Logits have to stay below 2^30 in magnitude (loss and lse mean nothing
+ * beyond); one of minus infinity has no probability, any other that is not finite makes its token's loss NaN.  The results are the same from
+ * run to run.
  * M, N <= 2^22, K <= 2^20, ldx, ldw <= 2^21 and M / 256 * N / 256 <= 2^23, rounded up (MP8_ERR_UNSUPPORTED beyond).  A zero dimension is
  * valid and does nothing.
  */

@@ -110,3 +110,31 @@ def test_as_many_logits_as_a_launch_takes(mp8, M, N, K):
     tiles.within(lse[rows], want["lse"], want["dlse"], "lse")
     tiles.within(loss[rows], want["loss"], want["loss"] * (want["r"] + 4 * U) + 1e-44, "loss")
     assert bool((loss >= 0).all()) and bool(((lse > 0) & (lse < 100)).all())  # (every token has been written)
+
+
+@pytest.mark.parametrize("common", [0.0, 2.0 ** 10, -2.0 ** 14, 2.0 ** 17])
+def test_gradient_of_logits_with_a_common_part(mp8, common):
+    """The gradient's probabilities are exp(z - lse) with lse, its product with log2 e and their difference from the token weight's exponent in
+    FP32: 3 U |lse|, and 64 U for a shift of up to 64, beside what the loss has (the target's comes from the loss itself)."""
+    M, N = 130, 700
+    rng = np.random.default_rng(N)
+    x, w = np.zeros((M, 8)), np.zeros((N, 8))
+    x[:, 0], w[:, 0] = 512.0, common / 512.0
+    x[:, 1:3] = rng.integers(-2, 3, (M, 2))
+    w[:, 1:3] = rng.integers(-64, 65, (N, 2)) / 64.0
+    t = rng.integers(0, N, M)
+    c = tokens(x, w, t)
+    z = x @ w.T
+    lse = z.max(1) + np.log(np.exp(z - z.max(1)[:, None]).sum(1))
+    loss = truth(c)["loss"]
+    e = np.exp(z - lse[:, None])
+    e[np.arange(M), t] = np.expm1(-loss)
+    r = (2 * math.log(2) * ((z.max(1) - z.min(1)) / math.log(2) + 1) + 64 + N / 32 + 16) * U
+    de = (H + r + 64 * U + 3 * U * np.abs(lse))[:, None] * np.abs(e) + 2.0 ** -39
+    x, w = np.abs(x), np.abs(w)
+    dev = forward(mp8, c)
+    dx, dw = buffers(M, N, 8, torch.float16)
+    backward(mp8, c, *dev, dx16=dx[:M * 8], dw16=dw[:N * 8])
+    for got, want, bound, what in ((dx[:M * 8], e @ c["w"].astype(np.float64), de @ w + N * U * (np.abs(e) @ w), "dx"),
+                                   (dw[:N * 8], e.T @ c["x"].astype(np.float64), de.T @ x + M * U * (np.abs(e).T @ x), "dw")):
+        close(got, want, bound + H * (np.abs(want) + bound) + 2.0 ** -25, what)

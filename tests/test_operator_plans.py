@@ -17,3 +17,12 @@ def test_logits_in_one_launch(M, N, K):
     tiles = [t for t in (64, 128, 256) if -(-N // t) == parts]
     assert tiles and rest < 256
     assert -(-M // min(tiles)) * parts <= 1 << 23
+
+
+@pytest.mark.parametrize("M,N,K,share", [(8192, 131072, 2048, 32), (6007, 37003, 1000, 32), (4096, 32000, 512, 16), (1 << 17, 1 << 20, 64, 16),
+                                         (512, 1000, 64, 8), (1, 32000, 512, 8)])
+def test_forward_workspace_as_stated(M, N, K, share):
+    """M * N / 8 bytes, and M * N / 16 or / 32 where larger tiles are taken: up to one tile of classes more, beside the copy of x and four bytes
+    per token."""
+    need = mp8.softmax_xent_fwd_workspace_bytes(M, N, K) - up(2 * M * up(K, 64), 256) - up(4 * M, 256)
+    assert M * N // share <= need <= M * N // share + 8 * M + 256
