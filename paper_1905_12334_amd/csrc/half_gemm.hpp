@@ -38,7 +38,7 @@ struct HalfGemm {
     uint32_t *arrived;
     FastDiv div_tiles;   // by the tiles of one slice
     FastDiv div_splits;
-    FastDiv div_band, div_last, div_tn;  // by 8 * tiles_n, by the height of the last band of 8 tile rows, by tiles_n
+    FastDiv div_band, div_last;  // by 8 * tiles_n, by the height of the last band of 8 tile rows
 };
 
 // Which part of the output a workgroup makes.
@@ -481,11 +481,12 @@ __device__ __forceinline__ void half_wave_lds() {
 
 // Rows of halves through LDS, so that a store covers whole 128-byte lines (pieces of 32 bytes, as the accumulators lie, kept the L2 busy
 // for as long as four times their size: 8192 x 32768 halves in 256x256 tiles 9 us per round of tiles).  A band of 32 rows of a wave's
-// part takes WTN * 64 bytes; 16-byte chunk c of row r sits in slot c ^ (r & mask), and its halves change places in rows 16 .. 31, which
+// part takes WTN * 64 bytes; 16-byte chunk c of row r sits in slot c ^ (r & MASK), and its halves change places in rows 16 .. 31, which
 // keeps the lanes of a write apart.  LDS operations of a wave are done in order.
 template <class T>
 struct HalfLines {
-    static constexpr int PER = T::WTN / 8, MASK = (PER & (PER - 1)) == 0 ? PER - 1 : 3, ROWS = 64 / PER, PASSES = (32 + ROWS - 1) / ROWS;
+    static constexpr int PER = T::WTN / 8, MASK = PER - 1, ROWS = 64 / PER, PASSES = 32 / ROWS;
+    static_assert((PER & MASK) == 0, "the lanes of a row");
     uint8_t *band;
     int lane;
     __device__ __forceinline__ HalfLines(const HalfPlace<T> &at) : band(at.lds + at.wave * T::WTN * 64), lane(at.lane) {}
@@ -502,7 +503,6 @@ struct HalfLines {
 #pragma unroll
         for (int k = 0; k < PASSES; ++k) {
             const int r = ROWS * k + lr;
-            if (64 % PER != 0 && (lr >= ROWS || r >= 32)) continue;
             const u32x4 v = *reinterpret_cast<const u32x4 *>(band + r * T::WTN * 2 + ((c ^ (r & MASK)) << 4));
             f(r, 8 * c, r < 16 ? v : u32x4{v.z, v.w, v.x, v.y});
         }
@@ -577,11 +577,11 @@ struct HalfNoneAhead {
 // eight and at least the columns, so that whole groups of eight may be stored).
 struct HalfEpiSum : HalfNoneAhead {
     float *out;
-    int64_t ld, slab, batch;  // in floats
+    int64_t ld, slab;  // in floats
     int rows, cols, add;
     template <class T>
     __device__ __forceinline__ void operator()(const HalfPlace<T> &at, f32x16 (&acc)[T::MT][T::NT], HalfNothing) const {
-        float *base = out + at.batch * batch + at.split * slab;
+        float *base = out + at.split * slab;
         struct Eight {
             f32x4 lo, hi;
         };
@@ -677,7 +677,6 @@ static inline HalfGemm half_gemm_args(const HalfMatrix &a, const HalfMatrix &b, 
     p.div_splits = make_fastdiv((uint32_t)splits);
     p.div_band = make_fastdiv((uint32_t)(8 * p.tiles_n));
     p.div_last = make_fastdiv((uint32_t)(p.tiles_m % 8 ? p.tiles_m % 8 : 8));
-    p.div_tn = make_fastdiv((uint32_t)p.tiles_n);
     return p;
 }
 

@@ -615,7 +615,6 @@ mp8_status ortho_sizes(int64_t batch, int64_t rows, int64_t cols) {
     const int64_t side = (int64_t)1 << 20;
     if (rows > side || cols > side || batch > 65535) return MP8_ERR_UNSUPPORTED;
     if (batch * ((rows + 63) / 64) * ((cols + 63) / 64) > ((int64_t)1 << 23)) return MP8_ERR_UNSUPPORTED;
-    if ((rows + 63) / 64 > 65535 || (cols + 63) / 64 > 65535) return MP8_ERR_UNSUPPORTED;
     return MP8_OK;
 }
 

@@ -741,7 +741,7 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
             if (plans.dx_direct) {
                 if (!direct(std::false_type{}, plans.dx.tile, E, W, M, cols, 0, dx16, dx8, dx_offset, dx_stats)) return MP8_ERR_HIP;
             } else {
-                const HalfEpiSum sum{{}, dxs, s.Kp, M * s.Kp, 0, (int)M, (int)K, c != 0};
+                const HalfEpiSum sum{{}, dxs, s.Kp, M * s.Kp, (int)M, (int)K, c != 0};
                 if (!product<true, false>(plans.dx.tile, E, W, M, K8, cols, plans.dx.splits, sum, st)) return MP8_ERR_HIP;
             }
         }
@@ -749,7 +749,7 @@ extern "C" mp8_status mp8_softmax_xent_bwd_fp16(int64_t M, int64_t N, int64_t K,
             if (plans.dw_direct) {
                 if (!direct(std::true_type{}, plans.dw.tile, E, X, cols, M, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             } else {
-                const HalfEpiSum sum{{}, dws, s.Kp, s.piece * s.Kp, 0, (int)cols, (int)K, 0};
+                const HalfEpiSum sum{{}, dws, s.Kp, s.piece * s.Kp, (int)cols, (int)K, 0};
                 if (!product<true, true>(plans.dw.tile, E, X, up(cols, 8), K8, M, plans.dw.splits, sum, st)) return MP8_ERR_HIP;
                 if (!finish(dws, s.piece * s.Kp, plans.dw.splits, cols, c, dw16, dw8, dw_offset, dw_stats)) return MP8_ERR_HIP;
             }
