@@ -565,12 +565,18 @@ void update(Args a) {
         }), "mp8_adam_fp16_sr");
 }
 
-// Every tensor given lies on the current device, whose stream the call goes to.
+// Every tensor given lies on the current device, whose stream the call goes to, or in pinned host memory (where scratch, counters and flags are
+// taken as addresses, any tensor would pass otherwise, and the kernels would fault on its memory).
 void on_current_device(std::initializer_list<const Arg *> args) {
     const int current = c10::hip::current_device();
-    for (const Arg *x : args)
-        if (x->given && x->t != nullptr && x->t->is_cuda() && x->t->get_device() != current)
+    for (const Arg *x : args) {
+        if (!x->given || x->t == nullptr || x->t->numel() == 0) continue;
+        if (!x->t->is_cuda()) {
+            if (!x->t->is_pinned()) fail("a tensor lies in host memory that is not pinned");
+        } else if (x->t->get_device() != current) {
             fail("a tensor lies on another device than the current one");
+        }
+    }
 }
 
 // The operands both directions share.
